@@ -477,6 +477,15 @@ dx_status dx_pages_plan(dx_ctx *ctx, int B, int T, int page_size, int n_pages, i
                         int32_t *lens_out, int32_t *free_out, int32_t *q_offsets,
                         int32_t *slots, int32_t *positions, int32_t *status);
 
+/* dx_pages_plan on the state of a loop: lens and free_pages are both read and written, and a step that is
+ * accepted sets drops (or NULL) to 0, because its tokens have been taken back; a refused one leaves them for the
+ * next.  So a verification's drops count once, whether or not another one stands between two plans.
+ * (dx_pages_plan only reads its drops: planned twice with the same, the tokens go twice.) */
+dx_status dx_pages_plan_in_place(dx_ctx *ctx, int B, int T, int page_size, int n_pages, int table_stride,
+                                 const int32_t *new_lens, int32_t *lens, int32_t *drops, int32_t *free_pages,
+                                 int32_t *free_list, int32_t *table, int32_t *q_offsets, int32_t *slots,
+                                 int32_t *positions, int32_t *status);
+
 /* Keys and values of T tokens into the cache: k, v dev bf16, token t's kv heads at k + t * k_stride
  * (elements; rows of a fused projection are fine), slots dev int32 [T], distinct; a slot outside the
  * cache (-1) is skipped.  e4m3: the value divided by the head's scale (IEEE fp32), cut to +-448, rounded to

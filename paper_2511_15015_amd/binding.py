@@ -30,7 +30,7 @@ EXPORTS = [
     "dx_handle_table", "dx_get_handle", "dx_get_formats", "dx_get_states", "dx_get_counters", "dx_get_stats", "dx_get_pool",
     "dx_set_profiling", "dx_get_profile", "dx_probe_read",
     "dx_pools_create", "dx_expert_install", "dx_promote_async", "dx_demote_async", "dx_migrate_poll",
-    "dx_serve_reserve", "dx_pages_plan", "dx_kv_write", "dx_paged_attention", "dx_draft_verify",
+    "dx_serve_reserve", "dx_pages_plan", "dx_pages_plan_in_place", "dx_kv_write", "dx_paged_attention", "dx_draft_verify",
 ]
 
 
@@ -147,6 +147,7 @@ def load():
     i64, kv = C.c_int64, C.POINTER(DxKvCache)
     L.dx_serve_reserve.argtypes = [vp, i32, i32]
     L.dx_pages_plan.argtypes = [vp, i32, i32, i32, i32, i32] + [vp] * 12
+    L.dx_pages_plan_in_place.argtypes = [vp, i32, i32, i32, i32, i32] + [vp] * 10
     L.dx_kv_write.argtypes = [vp, kv, vp, i64, vp, i64, vp, i32]
     L.dx_paged_attention.argtypes = [vp, kv, vp, i64, i32, vp, vp, vp, i32, i32, i32, i32, C.c_float, i32, vp, i64, vp]
     L.dx_draft_verify.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp]
@@ -454,6 +455,19 @@ class Context:
                                    _i32(slots), _i32(positions), _i32(status))
         if s:
             self._chk(s, "dx_pages_plan")
+
+    def dx_pages_plan_in_place(self, new_lens, lens, drops, free, free_list, table, page_size, q_offsets, slots, positions, status):
+        """lens, free and drops (or None) are updated in place."""
+        B, stride = table.shape
+        T = slots.numel()
+        assert new_lens.numel() == lens.numel() == B and q_offsets.numel() == B + 1
+        assert drops is None or drops.numel() == B
+        assert positions.numel() == T and status.numel() == 4
+        s = self.lib.dx_pages_plan_in_place(self.h, B, T, page_size, free_list.numel(), stride, _i32(new_lens), _i32(lens), _i32(drops),
+                                            _i32(free), _i32(free_list), _i32(table), _i32(q_offsets), _i32(slots), _i32(positions),
+                                            _i32(status))
+        if s:
+            self._chk(s, "dx_pages_plan_in_place")
 
     def dx_kv_write(self, cache: DxKvCache, k, v, slots):
         """k, v bf16 [T, kv_heads, head_dim], rows at any stride (slices of a fused projection)."""

@@ -237,6 +237,7 @@ void dxk_tiles_down(const dx_fwd_args &a, hipStream_t s, hipEvent_t start, hipEv
 constexpr int DX_SERVE_MAX_REQUESTS = 4096;
 struct dx_plan_args {
     const int32_t *new_lens, *lens_in, *drops, *free_in; // drops may be null
+    int32_t *spent; // drops, set to 0 by an accepted step, or null
     int32_t *free_list, *table, *lens_out, *free_out, *q_offsets, *slots, *positions, *status;
     int B, T, page_shift, n_pages, stride;
 };

@@ -162,6 +162,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan(dx_plan_args a)
         const int b = tid * per + i;
         if (b >= a.B) break;
         a.lens_out[b] = fine ? s_base[b] + s_q[b + 1] - s_q[b] : a.lens_in[b];
+        if (a.spent && fine) a.spent[b] = 0; // (read by the same thread)
     }
     for (int b = tid; b <= a.B; b += kPlanThreads) a.q_offsets[b] = fine ? s_q[b] : 0;
     if (tid == 0) {
@@ -536,6 +537,24 @@ dx_status check_cache(dx_ctx *c, const char *who, const dx_kv_cache *k)
     return DX_OK;
 }
 
+dx_status plan(dx_ctx *c, const char *who, int page_size, dx_plan_args a)
+{
+    if (const dx_status s = reserved(c, who, a.B)) return s;
+    if (a.T < 0 || a.T > c->cfg.max_tokens) DX_FAIL(c, DX_ERR_INVALID, "%s: T=%d outside [0,%d]", who, a.T, c->cfg.max_tokens);
+    a.page_shift = page_shift(page_size);
+    if (a.page_shift < 0) DX_FAIL(c, DX_ERR_INVALID, "%s: page_size=%d is not 16, 32, 64, 128 or 256", who, page_size);
+    if (a.n_pages < 1 || (int64_t)a.n_pages * page_size > 0x7FFFFFFFLL)
+        DX_FAIL(c, DX_ERR_INVALID, "%s: n_pages=%d (of %d tokens) outside the range of 31-bit slots", who, a.n_pages, page_size);
+    if (a.stride < 1 || (int64_t)a.stride * page_size > 0x7FFFFFFFLL)
+        DX_FAIL(c, DX_ERR_INVALID, "%s: table_stride=%d (pages of %d tokens) outside the range", who, a.stride, page_size);
+    if (!a.free_in || !a.free_list || !a.free_out || !a.q_offsets || !a.status || (a.T > 0 && (!a.slots || !a.positions)) ||
+        (a.B > 0 && (!a.new_lens || !a.lens_in || !a.table || !a.lens_out)))
+        DX_FAIL(c, DX_ERR_INVALID, "%s: null pointer", who);
+    hipLaunchKernelGGL(k_plan, dim3(1), dim3(kPlanThreads), 0, c->compute, a);
+    DX_HIP(c, hipGetLastError());
+    return DX_OK;
+}
+
 } // namespace
 
 extern "C" dx_status dx_serve_reserve(dx_ctx *c, int max_requests, int max_head_dim)
@@ -572,22 +591,20 @@ extern "C" dx_status dx_pages_plan(dx_ctx *c, int B, int T, int page_size, int n
                                    int32_t *free_out, int32_t *q_offsets, int32_t *slots, int32_t *positions, int32_t *status)
 {
     if (!c) return DX_ERR_INVALID;
-    if (const dx_status s = reserved(c, "dx_pages_plan", B)) return s;
-    if (T < 0 || T > c->cfg.max_tokens) DX_FAIL(c, DX_ERR_INVALID, "dx_pages_plan: T=%d outside [0,%d]", T, c->cfg.max_tokens);
-    const int shift = page_shift(page_size);
-    if (shift < 0) DX_FAIL(c, DX_ERR_INVALID, "dx_pages_plan: page_size=%d is not 16, 32, 64, 128 or 256", page_size);
-    if (n_pages < 1 || (int64_t)n_pages * page_size > 0x7FFFFFFFLL)
-        DX_FAIL(c, DX_ERR_INVALID, "dx_pages_plan: n_pages=%d (of %d tokens) outside the range of 31-bit slots", n_pages, page_size);
-    if (table_stride < 1 || (int64_t)table_stride * page_size > 0x7FFFFFFFLL)
-        DX_FAIL(c, DX_ERR_INVALID, "dx_pages_plan: table_stride=%d (pages of %d tokens) outside the range", table_stride, page_size);
-    if (!free_in || !free_list || !free_out || !q_offsets || !status || (T > 0 && (!slots || !positions)) ||
-        (B > 0 && (!new_lens || !lens_in || !table || !lens_out)))
-        DX_FAIL(c, DX_ERR_INVALID, "dx_pages_plan: null pointer");
-    dx_plan_args a{new_lens, lens_in, drops, free_in, free_list, table, lens_out, free_out, q_offsets, slots, positions, status,
-                   B, T, shift, n_pages, table_stride};
-    hipLaunchKernelGGL(k_plan, dim3(1), dim3(kPlanThreads), 0, c->compute, a);
-    DX_HIP(c, hipGetLastError());
-    return DX_OK;
+    return plan(c, "dx_pages_plan", page_size,
+                dx_plan_args{new_lens, lens_in, drops, free_in, nullptr, free_list, table, lens_out, free_out, q_offsets, slots, positions,
+                             status, B, T, 0, n_pages, table_stride});
+}
+
+extern "C" dx_status dx_pages_plan_in_place(dx_ctx *c, int B, int T, int page_size, int n_pages, int table_stride,
+                                            const int32_t *new_lens, int32_t *lens, int32_t *drops, int32_t *free_pages,
+                                            int32_t *free_list, int32_t *table, int32_t *q_offsets, int32_t *slots,
+                                            int32_t *positions, int32_t *status)
+{
+    if (!c) return DX_ERR_INVALID;
+    return plan(c, "dx_pages_plan_in_place", page_size,
+                dx_plan_args{new_lens, lens, drops, free_pages, drops, free_list, table, lens, free_pages, q_offsets, slots, positions,
+                             status, B, T, 0, n_pages, table_stride});
 }
 
 extern "C" dx_status dx_kv_write(dx_ctx *c, const dx_kv_cache *cache, const void *k, int64_t k_stride, const void *v,

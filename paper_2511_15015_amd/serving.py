@@ -35,9 +35,10 @@ class PagedCache:
 
     def plan(self, new_lens, T: int):
         """Pages and slots of a step's T tokens, new_lens int32 [requests] on the device (-1: the request has ended).  What the
-        last verification left in ``drops`` is taken back first.  ``status`` tells a refused step."""
-        self.ctx.dx_pages_plan(new_lens, self.lens, self.drops, self.free, self.free_list, self.table, self.page_size, self.lens,
-                               self.free, self.q_offsets, self.slots[:T], self.positions[:T], self.status)
+        last verification left in ``drops`` is taken back first, once: an accepted step clears it.  ``status`` tells a refused
+        step, which changes nothing."""
+        self.ctx.dx_pages_plan_in_place(new_lens, self.lens, self.drops, self.free, self.free_list, self.table, self.page_size,
+                                        self.q_offsets, self.slots[:T], self.positions[:T], self.status)
 
     def write(self, layer: int, k, v):
         """k, v bf16 [T, kv_heads, head_dim] of the planned tokens (rows at any stride)."""

@@ -1,0 +1,148 @@
+"""Edges of the serving calls: state that is carried from step to step, refused steps, numbers at the ends of their ranges."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests import serving_reference as R
+from tests.test_gpu_serving import B, Case, context, ctx, dev, plan_outputs  # noqa: F401  (B and ctx: fixtures)
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- state from step to step ------------------------------------------------------------------------------------------
+def paged_cache(ctx, requests=3, n_pages=16, max_len=96):  # noqa: F811
+    from paper_2511_15015_amd.serving import PagedCache
+    return PagedCache(ctx, layers=1, requests=requests, max_tokens=64, max_len=max_len, n_pages=n_pages, page_size=16, kv_heads=1, head_dim=64)
+
+
+def refuse_all(cache, drafts, max_n=None):
+    """A verification that accepts nothing (p is 0 at every token); drafts: how many each request brings."""
+    requests, n = len(drafts), sum(drafts)
+    max_n = max(drafts) if max_n is None else max_n
+    tokens, accepted = dev(np.full((requests, max_n + 1), -7)), dev(np.full(requests, -7))
+    p, u = torch.zeros((n + requests, 8), device="cuda"), torch.full((n + requests,), 0.5, device="cuda")
+    cache.verify(p, None, dev(np.zeros(n)), dev(np.concatenate([[0], np.cumsum(drafts)])), max_n, u[:n], u[n:], tokens, accepted)
+    return tokens, accepted
+
+
+def plan_of(cache, new, state, drops):
+    """cache.plan against the reference; -> its state"""
+    T = sum(max(n, 0) for n in new)
+    want = R.plan(cache.page_size, T, cache.free_list.numel(), np.array(new), state["lens"], np.array(drops), int(state["free"][0]),
+                  state["free_list"], state["table"])
+    cache.plan(dev(new), T)
+    torch.cuda.synchronize()
+    for name in ("lens", "free", "free_list", "table", "q_offsets", "status"):
+        assert np.array_equal(getattr(cache, name).cpu().numpy(), want[name]), (name, getattr(cache, name), want[name])
+    assert np.array_equal(cache.slots[:T].cpu().numpy(), want["slots"]) and np.array_equal(cache.positions[:T].cpu().numpy(), want["positions"])
+    return want
+
+
+def state_of(cache):
+    return {k: getattr(cache, k).cpu().numpy().astype(int) for k in ("lens", "free", "free_list", "table")}
+
+
+def test_dropped_tokens_are_taken_back_once(ctx):  # noqa: F811
+    """Steps without a verification behind one that left drops: each of them sees the drops of the verification before it, once."""
+    c = paged_cache(ctx)
+    s = plan_of(c, [18, 5, 20], state_of(c), [0, 0, 0])
+    refuse_all(c, [2, 0, 3])
+    assert c.drops.tolist() == [2, 0, 3]
+    s = plan_of(c, [1, 1, 0], s, [2, 0, 3])
+    assert c.drops.tolist() == [0, 0, 0]
+    s = plan_of(c, [1, 1, 1], s, [0, 0, 0])
+    s = plan_of(c, [0, 0, 0], s, [0, 0, 0])
+    assert c.lens.tolist() == [18, 7, 18]
+
+
+def test_a_place_is_taken_again_after_a_request_that_ended_with_drops(ctx):  # noqa: F811
+    c = paged_cache(ctx)
+    s = plan_of(c, [18, 5, 20], state_of(c), [0, 0, 0])
+    refuse_all(c, [1, 3, 0])
+    s = plan_of(c, [-1, -1, 1], s, [1, 3, 0])
+    s = plan_of(c, [5, 2, 1], s, [0, 0, 0])
+    assert c.status.tolist()[2:] == [0, 0] and c.lens.tolist() == [5, 2, 22]
+
+
+def test_drops_are_kept_by_a_step_that_is_refused(ctx):  # noqa: F811
+    c = paged_cache(ctx, requests=2, n_pages=4)
+    s = plan_of(c, [20, 32], state_of(c), [0, 0])
+    refuse_all(c, [2, 0])
+    s = plan_of(c, [1, 1], s, [2, 0])                            # a page is missing
+    assert c.status.tolist()[2] == 1 and c.drops.tolist() == [2, 0]
+    s = plan_of(c, [1, -1], s, [2, 0])
+    assert c.lens.tolist() == [19, 0] and c.drops.tolist() == [0, 0]
+
+
+def test_drops_of_a_plan_with_outputs_of_its_own_stay(ctx):  # noqa: F811
+    """dx_pages_plan reads its drops (several caches may share them, a step may be planned twice)."""
+    o, fl, tb = plan_outputs(1, 3), dev(np.arange(4)), dev([[3, -1]])
+    new, lens, drops, free = dev([3]), dev([9]), dev([2]), dev([3])
+    for _ in range(2):
+        ctx.dx_pages_plan(new, lens, drops, free, fl, tb, 16, o["lens"], o["free"], o["q_offsets"], o["slots"], o["positions"], o["status"])
+        assert o["lens"].tolist() == [10] and drops.tolist() == [2] and o["slots"].tolist() == [55, 56, 57]
+
+
+def test_drops_in_replays_of_a_graph(B):  # noqa: F811
+    """A captured step whose verification leaves drops for the next replay's plan, beside eager steps without a verification."""
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        c = paged_cache(context(B, stream.cuda_stream), max_len=96, n_pages=30)
+        new, drafts, V = dev([0, 0, 0]), 3, 8
+        p, u = torch.zeros((3 * drafts + 3, V), device="cuda"), torch.full((3 * drafts + 3,), 0.5, device="cuda")
+        offsets, draft = dev(np.arange(4) * drafts), dev(np.zeros(3 * drafts))
+        tokens, accepted = dev(np.zeros((3, drafts + 1))), dev(np.zeros(3))
+
+        def step():
+            c.plan(new, 12)
+            c.verify(p, None, draft, offsets, drafts, u[:9], u[9:], tokens, accepted)
+
+        def start():
+            for t in (c.lens, c.drops):
+                t.zero_()
+            c.free.fill_(30)
+            c.free_list.copy_(torch.arange(30))
+
+        step()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        start()
+        with torch.cuda.graph(g, stream=stream):
+            step()
+        rng = np.random.default_rng(2)
+        start()
+        lens, drops = np.zeros(3, int), np.zeros(3, int)
+        for i in range(12):
+            new.copy_(dev([4, 4, 4]))
+            good = [int(x) for x in rng.integers(0, drafts + 1, 3)]          # drafts to accept
+            p.zero_()
+            for b in range(3):
+                p[b * (drafts + 1):b * (drafts + 1) + good[b], 0] = 1
+            g.replay()
+            torch.cuda.synchronize()
+            lens, drops = lens - drops + 4, drafts - np.array(good)
+            assert c.status.tolist()[2:] == [0, 0] and c.lens.tolist() == lens.tolist() and c.drops.tolist() == drops.tolist()
+            if i % 3 == 1:                                                   # a chunk with nothing to judge
+                n = [int(x) for x in rng.integers(0, 4, 3)]
+                c.plan(dev(n), sum(n))
+                torch.cuda.synchronize()
+                lens, drops = lens - drops + n, drops * 0
+                assert c.lens.tolist() == lens.tolist() and c.drops.tolist() == [0, 0, 0]
+        c.ctx.close()
+
+
+def test_refusals_of_planning_in_place(B, ctx):  # noqa: F811
+    p = dev(np.zeros(64)).data_ptr()
+
+    def plan(n=1, T=1, P=16, n_pages=4, stride=2, new=p, lens=p, drops=p, free=p, status=p):
+        return ctx.lib.dx_pages_plan_in_place(ctx.h, n, T, P, n_pages, stride, new, lens, drops, free, p, p, p, p, p, status)
+
+    for kw, word in (({"n": 1501}, "B="), ({"n": -1}, "B="), ({"T": -1}, "T="), ({"P": 8}, "page_size"), ({"n_pages": 0}, "n_pages"), ({"stride": 0}, "table_stride"),
+                     ({"n_pages": 1 << 27}, "n_pages"), ({"new": None}, "null"), ({"lens": None}, "null"), ({"free": None}, "null"), ({"status": None}, "null")):
+        assert plan(**kw) == B.DX_ERR_INVALID
+        text = ctx.lib.dx_last_error(ctx.h).decode()
+        assert text.startswith("dx_pages_plan_in_place") and word in text, text
+
+
