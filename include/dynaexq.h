@@ -468,7 +468,8 @@ dx_status dx_serve_reserve(dx_ctx *ctx, int max_requests, int max_head_dim);
  *                 more than table_stride pages, 2^22 pages or new tokens, a returned page that is none, more than T tokens)
  * If pages are missing or a request is bad the step is refused as a whole: free_list and table stay as they
  * are, lens_out = lens_in, free_out = free_in, q_offsets all 0, slots and positions all -1, status[0] and
- * status[1] 0 -- and the calls below, given these arrays, do nothing.
+ * status[1] 0 -- and dx_kv_write, dx_paged_attention and dx_draft_verify_planned, given these arrays, do
+ * nothing (dx_draft_verify does not know of the step).
  * 0 <= B <= max_requests of dx_serve_reserve, 0 <= T <= max_tokens of the context, table_stride * page_size and
  * n_pages * page_size below 2^31. */
 dx_status dx_pages_plan(dx_ctx *ctx, int B, int T, int page_size, int n_pages, int table_stride,
@@ -530,6 +531,13 @@ dx_status dx_paged_attention(dx_ctx *ctx, const dx_kv_cache *cache, const void *
 dx_status dx_draft_verify(dx_ctx *ctx, const float *p, const float *q, const int32_t *draft, const int32_t *offsets,
                           int B, int n_drafts, int max_n, int V, const float *u_accept, const float *u_sample,
                           int32_t *tokens, int32_t *accepted, int32_t *drops);
+
+/* dx_draft_verify for a step that dx_pages_plan has planned; status: dev, as it wrote it.  If the step was refused (pages
+ * missing or a bad request) its tokens were not written and p is of nothing: tokens are all -1, accepted 0, and drops stay as they
+ * are, those of the step before, which the refused plan has not taken back either. */
+dx_status dx_draft_verify_planned(dx_ctx *ctx, const int32_t *status, const float *p, const float *q, const int32_t *draft,
+                                  const int32_t *offsets, int B, int n_drafts, int max_n, int V, const float *u_accept,
+                                  const float *u_sample, int32_t *tokens, int32_t *accepted, int32_t *drops);
 
 #ifdef __cplusplus
 }

@@ -31,6 +31,7 @@ EXPORTS = [
     "dx_set_profiling", "dx_get_profile", "dx_probe_read",
     "dx_pools_create", "dx_expert_install", "dx_promote_async", "dx_demote_async", "dx_migrate_poll",
     "dx_serve_reserve", "dx_pages_plan", "dx_pages_plan_in_place", "dx_kv_write", "dx_paged_attention", "dx_draft_verify",
+    "dx_draft_verify_planned",
 ]
 
 
@@ -151,6 +152,7 @@ def load():
     L.dx_kv_write.argtypes = [vp, kv, vp, i64, vp, i64, vp, i32]
     L.dx_paged_attention.argtypes = [vp, kv, vp, i64, i32, vp, vp, vp, i32, i32, i32, i32, C.c_float, i32, vp, i64, vp]
     L.dx_draft_verify.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp]
+    L.dx_draft_verify_planned.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp]
     _lib = L
     return L
 
@@ -195,6 +197,17 @@ def _rows(t, T, heads, D):
     assert t.shape == (T, heads, D) and t.dtype is _bfloat16
     assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == D), "heads and channels must be contiguous"
     return t.data_ptr(), t.stride(0) if T > 1 else heads * D
+
+
+def _drafts(p, q, draft, offsets, max_n, u_accept, u_sample, tokens, accepted, drops):
+    """Arguments of a verification from its tensors."""
+    B, n, V = u_sample.numel(), draft.numel(), p.shape[1]
+    assert p.shape[0] == n + B and offsets.numel() == B + 1 and u_accept.numel() == n
+    assert q is None or q.shape == (n, V)
+    assert tokens.shape == (B, max_n + 1) and accepted.numel() == B and (drops is None or drops.numel() == B)
+    # (no drafts: q is an empty tensor, which has no address)
+    return (_f32(p), _f32(q), _i32(draft), _i32(offsets), B, n, max_n, V, _f32(u_accept), _f32(u_sample), _i32(tokens), _i32(accepted),
+            _i32(drops))
 
 
 def make_kv_cache(k, v, k_scale=None, v_scale=None) -> DxKvCache:
@@ -492,15 +505,17 @@ class Context:
 
     def dx_draft_verify(self, p, q, draft, offsets, max_n, u_accept, u_sample, tokens, accepted, drops=None):
         """p fp32 [n_drafts + B, V], q fp32 [n_drafts, V] or None, tokens int32 [B, max_n + 1]."""
-        B, n, V = u_sample.numel(), draft.numel(), p.shape[1]
-        assert p.shape[0] == n + B and offsets.numel() == B + 1 and u_accept.numel() == n
-        assert q is None or q.shape == (n, V)
-        assert tokens.shape == (B, max_n + 1) and accepted.numel() == B and (drops is None or drops.numel() == B)
-        # (no drafts: q is an empty tensor, which has no address)
-        s = self.lib.dx_draft_verify(self.h, _f32(p), _f32(q), _i32(draft), _i32(offsets), B, n, max_n, V, _f32(u_accept),
-                                     _f32(u_sample), _i32(tokens), _i32(accepted), _i32(drops))
+        s = self.lib.dx_draft_verify(self.h, *_drafts(p, q, draft, offsets, max_n, u_accept, u_sample, tokens, accepted, drops))
         if s:
             self._chk(s, "dx_draft_verify")
+
+    def dx_draft_verify_planned(self, status, p, q, draft, offsets, max_n, u_accept, u_sample, tokens, accepted, drops=None):
+        """dx_draft_verify of a step whose plan wrote status [4]: a refused one is not judged."""
+        assert status.numel() == 4
+        s = self.lib.dx_draft_verify_planned(self.h, _i32(status),
+                                             *_drafts(p, q, draft, offsets, max_n, u_accept, u_sample, tokens, accepted, drops))
+        if s:
+            self._chk(s, "dx_draft_verify_planned")
 
     def dx_migrate_poll(self, wait=False) -> int:
         n = C.c_int(0)

@@ -320,6 +320,7 @@ struct verify_args {
     const int32_t *draft, *offsets;
     const float *u_accept, *u_sample;
     int32_t *tokens, *accepted, *drops; // drops may be null
+    const int32_t *status;              // of the step's plan, or null
     int B, n_drafts, max_n, V;
     unsigned long long *sums; // [B, kSums], 0 between calls: of a request's chunks (and kStored), from kCount on how many there are
 };
@@ -427,6 +428,13 @@ __global__ __launch_bounds__(kVerifyThreads) void k_verify(verify_args a)
     __shared__ int s_found, s_last;
     const int b = blockIdx.y, chunks = gridDim.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     unsigned long long *const sums = a.sums + (long)b * kSums;
+    if (a.status && (a.status[2] | a.status[3])) { // there was no step: p is of no tokens
+        if (blockIdx.x == 0) {
+            for (int i = tid; i <= a.max_n; i += kVerifyThreads) a.tokens[(long)b * (a.max_n + 1) + i] = -1;
+            if (tid == 0) a.accepted[b] = 0;
+        }
+        return;
+    }
     const verdict r = judge(a, b);
     const rest s(a, b, r);
     double sum = 0.; // exact: 4096 whole numbers of up to 2^39
@@ -551,6 +559,22 @@ dx_status plan(dx_ctx *c, const char *who, int page_size, dx_plan_args a)
         (a.B > 0 && (!a.new_lens || !a.lens_in || !a.table || !a.lens_out)))
         DX_FAIL(c, DX_ERR_INVALID, "%s: null pointer", who);
     hipLaunchKernelGGL(k_plan, dim3(1), dim3(kPlanThreads), 0, c->compute, a);
+    DX_HIP(c, hipGetLastError());
+    return DX_OK;
+}
+
+dx_status verify(dx_ctx *c, const char *who, verify_args a)
+{
+    if (const dx_status s = reserved(c, who, a.B)) return s;
+    if (a.V < 1 || a.V > 1 << 20) DX_FAIL(c, DX_ERR_INVALID, "%s: V=%d outside [1,2^20]", who, a.V);
+    if (a.max_n < 0 || a.max_n > 255) DX_FAIL(c, DX_ERR_INVALID, "%s: max_n=%d outside [0,255]", who, a.max_n);
+    if (a.n_drafts < 0 || (int64_t)a.n_drafts > (int64_t)a.B * a.max_n)
+        DX_FAIL(c, DX_ERR_INVALID, "%s: n_drafts=%d outside [0, B * max_n]", who, a.n_drafts);
+    if (a.B == 0) return DX_OK;
+    if (!a.p || !a.offsets || !a.u_sample || !a.tokens || !a.accepted || (a.n_drafts > 0 && (!a.draft || !a.u_accept)))
+        DX_FAIL(c, DX_ERR_INVALID, "%s: null pointer", who);
+    a.sums = reinterpret_cast<unsigned long long *>(c->serve_scratch + c->verify_scratch);
+    hipLaunchKernelGGL(k_verify, dim3((a.V + kChunk - 1) / kChunk, a.B), dim3(kVerifyThreads), 0, c->compute, a);
     DX_HIP(c, hipGetLastError());
     return DX_OK;
 }
@@ -686,17 +710,15 @@ extern "C" dx_status dx_draft_verify(dx_ctx *c, const float *p, const float *q, 
                                      int32_t *tokens, int32_t *accepted, int32_t *drops)
 {
     if (!c) return DX_ERR_INVALID;
-    if (const dx_status s = reserved(c, "dx_draft_verify", B)) return s;
-    if (V < 1 || V > 1 << 20) DX_FAIL(c, DX_ERR_INVALID, "dx_draft_verify: V=%d outside [1,2^20]", V);
-    if (max_n < 0 || max_n > 255) DX_FAIL(c, DX_ERR_INVALID, "dx_draft_verify: max_n=%d outside [0,255]", max_n);
-    if (n_drafts < 0 || (int64_t)n_drafts > (int64_t)B * max_n)
-        DX_FAIL(c, DX_ERR_INVALID, "dx_draft_verify: n_drafts=%d outside [0, B * max_n]", n_drafts);
-    if (B == 0) return DX_OK;
-    if (!p || !offsets || !u_sample || !tokens || !accepted || (n_drafts > 0 && (!draft || !u_accept)))
-        DX_FAIL(c, DX_ERR_INVALID, "dx_draft_verify: null pointer");
-    verify_args a{p, q, draft, offsets, u_accept, u_sample, tokens, accepted, drops, B, n_drafts, max_n, V,
-                  reinterpret_cast<unsigned long long *>(c->serve_scratch + c->verify_scratch)};
-    hipLaunchKernelGGL(k_verify, dim3((V + kChunk - 1) / kChunk, B), dim3(kVerifyThreads), 0, c->compute, a);
-    DX_HIP(c, hipGetLastError());
-    return DX_OK;
+    return verify(c, "dx_draft_verify", verify_args{p, q, draft, offsets, u_accept, u_sample, tokens, accepted, drops, nullptr, B, n_drafts, max_n, V});
+}
+
+extern "C" dx_status dx_draft_verify_planned(dx_ctx *c, const int32_t *status, const float *p, const float *q, const int32_t *draft,
+                                             const int32_t *offsets, int B, int n_drafts, int max_n, int V, const float *u_accept,
+                                             const float *u_sample, int32_t *tokens, int32_t *accepted, int32_t *drops)
+{
+    if (!c) return DX_ERR_INVALID;
+    if (!status) DX_FAIL(c, DX_ERR_INVALID, "dx_draft_verify_planned: null status");
+    return verify(c, "dx_draft_verify_planned",
+                  verify_args{p, q, draft, offsets, u_accept, u_sample, tokens, accepted, drops, status, B, n_drafts, max_n, V});
 }

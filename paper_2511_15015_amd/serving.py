@@ -49,5 +49,6 @@ class PagedCache:
         self.ctx.dx_paged_attention(self.caches[layer], q, self.q_offsets, self.lens, self.table, max_q, scale, window, out, lse)
 
     def verify(self, p, q, draft, offsets, max_n: int, u_accept, u_sample, tokens, accepted):
-        """Accepts drafts (all arrays as for ``dx_draft_verify``); the next ``plan`` drops the others."""
-        self.ctx.dx_draft_verify(p, q, draft, offsets, max_n, u_accept, u_sample, tokens, accepted, self.drops)
+        """Accepts drafts of the step planned last (all arrays as for ``dx_draft_verify``); the next ``plan`` drops the others.  A
+        refused step gets no tokens, and the drops that its plan has not taken back stay."""
+        self.ctx.dx_draft_verify_planned(self.status, p, q, draft, offsets, max_n, u_accept, u_sample, tokens, accepted, self.drops)

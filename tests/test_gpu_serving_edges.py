@@ -146,3 +146,62 @@ def test_refusals_of_planning_in_place(B, ctx):  # noqa: F811
         assert text.startswith("dx_pages_plan_in_place") and word in text, text
 
 
+def test_a_refused_step_leaves_drops_and_verdicts_of_the_step_before(ctx):  # noqa: F811
+    """Drops are waiting, a step lacks pages and goes through attention and verification all the same, a request ends, the step is
+    taken again: lengths and pages as if it had not been tried."""
+    ends = []
+    for tried in (False, True):
+        c = paged_cache(ctx, requests=2, n_pages=4)
+        s = plan_of(c, [20, 32], state_of(c), [0, 0])
+        s = plan_of(c, [3, 0], s, [0, 0])
+        refuse_all(c, [2, 0])
+        if tried:
+            s = plan_of(c, [3, 1], s, [2, 0])
+            assert c.status.tolist()[2] == 1
+            q, out = torch.randn((4, 1, 64), device="cuda").to(torch.bfloat16), torch.full((4, 1, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+            k = c.k.clone()
+            c.write(0, q, q)
+            c.attend(0, q, out, 3, 0.1)
+            assert (out == 7).all() and torch.equal(k, c.k)
+            tokens, accepted = refuse_all(c, [1, 0])
+            assert c.drops.tolist() == [2, 0] and accepted.tolist() == [0, 0] and (tokens == -1).all()
+        s = plan_of(c, [3, -1], s, [2, 0])
+        tokens, accepted = refuse_all(c, [2, 0])
+        assert c.drops.tolist() == [2, 0] and (tokens[:, 0] >= 0).all()
+        s = plan_of(c, [1, 0], s, [2, 0])
+        ends.append({k: v.tolist() for k, v in state_of(c).items()})
+    assert ends[0]["lens"] == [23, 0] and ends[0] == ends[1]
+
+
+def test_verification_behind_an_accepted_plan(ctx):  # noqa: F811
+    """dx_draft_verify_planned and dx_draft_verify say the same where the step was accepted; what is refused writes nothing else."""
+    rng = np.random.default_rng(7)
+    ns, V = [3, 0, 2, 4], 9001
+    n, rows = sum(ns), sum(ns) + len(ns)
+    p, q = (torch.softmax(3 * torch.from_numpy(rng.standard_normal((x, V)).astype(np.float32)).cuda(), 1) for x in (rows, n))
+    draft, offsets, u = dev(rng.integers(0, V, n)), dev(np.concatenate([[0], np.cumsum(ns)])), torch.rand(rows, device="cuda")
+    for status in ([5, 6, 0, 0], [0, 0, 1, 0], [0, 0, 0, 2], [5, 6, 0, 0]):
+        outs = []
+        for call in (ctx.dx_draft_verify, lambda *a: ctx.dx_draft_verify_planned(dev(status), *a)):
+            o = [dev(np.full(s, -7)) for s in ((4, 5), 4, 4)]
+            call(p, q, draft, offsets, 4, u[:n], u[n:], *o)
+            outs.append([t.tolist() for t in o])
+        if status[2:] == [0, 0]:
+            assert outs[0] == outs[1]
+        else:
+            assert outs[1] == [[[-1] * 5] * 4, [0] * 4, [-7] * 4]
+
+
+def test_refusals_of_verification_behind_a_plan(B, ctx):  # noqa: F811
+    p, f = dev(np.zeros(64)).data_ptr(), torch.zeros(64, device="cuda").data_ptr()
+
+    def verify(status=p, n=1, drafts=1, most=1, V=8, pp=f, draft=p):
+        return ctx.lib.dx_draft_verify_planned(ctx.h, status, pp, f, draft, p, n, drafts, most, V, f, f, p, p, None)
+
+    for kw, word in (({"status": None}, "status"), ({"n": -1}, "B="), ({"V": 0}, "V="), ({"most": 256}, "max_n"), ({"drafts": 2}, "n_drafts"),
+                     ({"pp": None}, "null"), ({"draft": None}, "null")):
+        assert verify(**kw) == B.DX_ERR_INVALID
+        text = ctx.lib.dx_last_error(ctx.h).decode()
+        assert text.startswith("dx_draft_verify_planned") and word in text, text
+
+
