@@ -527,14 +527,17 @@ dx_status dx_paged_attention(dx_ctx *ctx, const dx_kv_cache *cache, const void *
  * that no order of summation can change it; if W = 0, the lowest v of the largest p_v (0 if there is none).
  *   tokens int32 [B, max_n + 1]: the accepted drafts, the drawn token, then -1; accepted int32 [B]: a;
  *   drops int32 [B] or NULL: n - a, what dx_pages_plan takes as drops
- * 1 <= V <= 2^20, 0 <= B <= max_requests, 0 <= max_n <= 255 (more drafts of a request are ignored). */
+ * 1 <= V <= 2^20, 0 <= B <= max_requests, 0 <= max_n <= 255, n_drafts <= B * max_n.  Of a request that brings more than max_n drafts the first
+ * max_n are judged, n is max_n, and drops does not count the others: a caller that has appended them to the cache adds
+ * them, or uses dx_draft_verify_planned, which does. */
 dx_status dx_draft_verify(dx_ctx *ctx, const float *p, const float *q, const int32_t *draft, const int32_t *offsets,
                           int B, int n_drafts, int max_n, int V, const float *u_accept, const float *u_sample,
                           int32_t *tokens, int32_t *accepted, int32_t *drops);
 
 /* dx_draft_verify for a step that dx_pages_plan has planned; status: dev, as it wrote it.  If the step was refused (pages
  * missing or a bad request) its tokens were not written and p is of nothing: tokens are all -1, accepted 0, and drops stay as they
- * are, those of the step before, which the refused plan has not taken back either. */
+ * are, those of the step before, which the refused plan has not taken back either.  All of the step's drafts are in
+ * the cache, so drops counts those behind the first max_n, too: it is offsets[b+1] - offsets[b] - a. */
 dx_status dx_draft_verify_planned(dx_ctx *ctx, const int32_t *status, const float *p, const float *q, const int32_t *draft,
                                   const int32_t *offsets, int B, int n_drafts, int max_n, int V, const float *u_accept,
                                   const float *u_sample, int32_t *tokens, int32_t *accepted, int32_t *drops);

@@ -326,7 +326,8 @@ struct verify_args {
 };
 
 struct verdict {
-    int first, n, a; // first draft of the request, drafts, accepted ones
+    int first, n, a; // first draft of the request, drafts that are judged, accepted ones
+    int brought;     // drafts of which those not accepted are dropped
 };
 
 // (offsets outside the arrays are cut to them)
@@ -337,6 +338,7 @@ __device__ verdict drafts_of(const verify_args &a, int b)
     r.first = lo;
     r.n = min(hi - lo, a.max_n);
     r.a = r.n;
+    r.brought = a.status ? hi - lo : r.n;
     return r;
 }
 
@@ -508,7 +510,7 @@ __global__ __launch_bounds__(kVerifyThreads) void k_verify(verify_args a)
         a.tokens[(long)b * (a.max_n + 1) + i] = i < r.a ? a.draft[r.first + i] : i == r.a ? token : -1;
     if (tid == 0) {
         a.accepted[b] = r.a;
-        if (a.drops) a.drops[b] = r.n - r.a;
+        if (a.drops) a.drops[b] = r.brought - r.a;
     }
 }
 

@@ -205,3 +205,17 @@ def test_refusals_of_verification_behind_a_plan(B, ctx):  # noqa: F811
         assert text.startswith("dx_draft_verify_planned") and word in text, text
 
 
+def test_drafts_beyond_the_most_are_dropped_too(ctx):  # noqa: F811
+    """The step has appended every draft: those behind the first max_n are not judged, and the next plan takes them back."""
+    c = paged_cache(ctx)
+    s = plan_of(c, [18, 5, 20], state_of(c), [0, 0, 0])
+    tokens, accepted = refuse_all(c, [4, 1, 1], max_n=2)             # all refused
+    assert accepted.tolist() == [0, 0, 0] and c.drops.tolist() == [4, 1, 1]
+    s = plan_of(c, [5, 1, 1], s, [4, 1, 1])
+    p, u = torch.ones((7, 8), device="cuda"), torch.full((7,), 0.5, device="cuda")
+    tokens, accepted = dev(np.zeros((3, 3))), dev(np.zeros(3))
+    c.verify(p, None, dev([1, 2, 3, 4]), dev([0, 4, 4, 4]), 2, u[:4], u[4:], tokens, accepted)   # all that are judged accepted
+    assert accepted.tolist() == [2, 0, 0] and tokens[0, :2].tolist() == [1, 2] and c.drops.tolist() == [2, 0, 0]
+    plan_of(c, [1, 0, 0], s, [2, 0, 0])
+
+
