@@ -463,7 +463,8 @@ dx_status dx_serve_reserve(dx_ctx *ctx, int max_requests, int max_head_dim);
  *   lens_out [B] lens_in - drops + new_lens (0 if ended), free_out [1]: may be lens_in and free_in
  *   q_offsets [B+1] exclusive prefix sum of max(new_lens, 0)
  *   slots, positions [T]: where each new token goes in the cache and its position in its request; -1 past
- *                 q_offsets[B] (T may be larger than the number of new tokens)
+ *                 q_offsets[B] (T may be larger than the number of new tokens); the slot is -1, too, if the page that the table
+ *                 or the free list names for it is none (outside 0 .. n_pages-1)
  *   status [4]: pages taken, pages returned, pages missing, bad requests (negative or too large numbers, a row of
  *                 more than table_stride pages, 2^22 pages or new tokens, a returned page that is none, more than T tokens)
  * If pages are missing or a request is bad the step is refused as a whole: free_list and table stay as they

@@ -181,7 +181,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan(dx_plan_args a)
             [&](int b, int i, int page) {
                 const int pos = s_base[b] + i, t = s_q[b] + i;
                 a.positions[t] = pos;
-                a.slots[t] = (page << a.page_shift) + (pos & ((1 << a.page_shift) - 1));
+                a.slots[t] = (uint32_t)page < (uint32_t)a.n_pages ? (page << a.page_shift) + (pos & ((1 << a.page_shift) - 1)) : -1;
             });
     for (int t = n_real + tid; t < a.T; t += kPlanThreads) a.slots[t] = a.positions[t] = -1;
 }

@@ -219,3 +219,19 @@ def test_drafts_beyond_the_most_are_dropped_too(ctx):  # noqa: F811
     plan_of(c, [1, 0, 0], s, [2, 0, 0])
 
 
+@pytest.mark.parametrize("page", [-1, -(1 << 27), 40, 1 << 27, (1 << 27) + 3, 1 << 28, 2 ** 31 - 1])
+def test_plan_gives_no_slot_in_a_page_that_is_none(ctx, page):  # noqa: F811
+    """A table entry that the step keeps, or a free page, that is no page of the cache: its tokens get no slot, and no one else's."""
+    for where in ("kept", "free"):
+        o, fl, tb = plan_outputs(2, 9), dev(np.arange(40)), dev([[7, -1], [8, -1]])
+        if where == "kept":
+            tb[0, 0] = page
+        else:
+            fl[39] = page                                       # the first one taken
+        new, lens = dev([5, 4]), dev([9, 16] if where == "kept" else [16, 9])
+        ctx.dx_pages_plan(new, lens, None, dev([40]), fl, tb, 16, o["lens"], o["free"], o["q_offsets"], o["slots"], o["positions"], o["status"])
+        fine = [39 * 16 + i for i in range(4)] if where == "kept" else [8 * 16 + 9 + i for i in range(4)]
+        assert o["status"].tolist() == [1, 0, 0, 0] and o["slots"].tolist() == [-1] * 5 + fine
+        assert o["positions"].tolist() == ([9, 10, 11, 12, 13, 16, 17, 18, 19] if where == "kept" else [16, 17, 18, 19, 20, 9, 10, 11, 12])
+
+
