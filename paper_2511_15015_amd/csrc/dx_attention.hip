@@ -146,6 +146,10 @@ __device__ int capacity(const dx_attn_args &a) { return a.table_stride << a.page
 // x / a.group for 0 <= x < 2^31 (dxk_paged_attention)
 __device__ int by_group(const dx_attn_args &a, int x) { return a.group == 1 ? x : (int)(__umulhi((uint32_t)x, a.group_mul) >> a.group_shift); }
 
+// first key of a window's that a row at pos sees (a position below 0, of a row that sees nothing, less a window that is as long as the type allows
+// would leave it)
+__device__ int window_from(const dx_attn_args &a, int pos) { return max(max(pos, 0) - a.window + 1, 0); }
+
 // The rows of a tile and the keys that they see.
 struct tile_rows {
     int token, first, rows; // first token of the request, first row of the tile in it, rows of the tile
@@ -167,8 +171,8 @@ __device__ tile_rows see(const dx_attn_args &a, const tokens &of, int first, int
     const int p0 = t.pos + by_group(a, first), p1 = t.pos + by_group(a, first + t.rows - 1);
     t.hi = max(min(min(p1 + 1, of.len), capacity(a)), 0);
     t.all_hi = min(p0 + 1, t.hi);
-    t.lo = a.window ? min(max(p0 - a.window + 1, 0), t.hi) : 0;
-    t.all_lo = a.window ? max(p1 - a.window + 1, 0) : 0;
+    t.lo = a.window ? min(window_from(a, p0), t.hi) : 0;
+    t.all_lo = a.window ? window_from(a, p1) : 0;
     return t;
 }
 
@@ -468,7 +472,7 @@ template <int D, bool FP8, int NT> struct queries {
             const int i = by_group(a, row), g = row - i * a.group;
             const DX_GLOBAL dx_bf16 *at = (const DX_GLOBAL dx_bf16 *)a.q + (long)(t.token + i) * a.q_stride + (long)(head * a.group + g) * D;
             k_max[n] = min(t.pos + i, t.hi - 1);
-            k_min[n] = a.window ? max(t.pos + i - a.window + 1, 0) : 0;
+            k_min[n] = a.window ? window_from(a, t.pos + i) : 0;
 #pragma unroll
             for (int s = 0; s < D / 32; ++s)
                 q[n][s] = *reinterpret_cast<const DX_GLOBAL u32x4 *>(at + (FP8 ? 64 * (s / 2) + 16 * grp + 8 * (s % 2) : 32 * s + 8 * grp));

@@ -235,3 +235,16 @@ def test_plan_gives_no_slot_in_a_page_that_is_none(ctx, page):  # noqa: F811
         assert o["positions"].tolist() == ([9, 10, 11, 12, 13, 16, 17, 18, 19] if where == "kept" else [16, 17, 18, 19, 20, 9, 10, 11, 12])
 
 
+# ---- numbers at the ends of their ranges ------------------------------------------------------------------------------
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 3, 1 << 30])
+def test_attention_window_of_any_size(B, ctx, window):  # noqa: F811
+    """A window that is no window, where the first tokens of a request have no keys (their positions are below zero)."""
+    for new in ([8, 1], [90, 3]):
+        for fmt in ("bf16", "fp8"):
+            c = Case(B, 8, 2, 64, 16, fmt, [100, 40], new, seed=1)
+            c.lens[0] = new[0] - 5
+            got = c.run(ctx, window)
+            c.check(got, window)
+            assert torch.isinf(got[1][:5]).all() and torch.isfinite(got[1][5:]).all()
+
+
