@@ -28,6 +28,7 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
 constexpr float kNothing = -1.7e38f; // maximum of a row that has seen no key yet
 constexpr float kRise = 8.f;
+constexpr float kFar = 16777216.f; // 2^24 (raise_maximum)
 constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
 
 __device__ uint32_t pack_bf16(float a, float b) // nearest even
@@ -524,8 +525,11 @@ template <int X, int N> __device__ void blank(u32x4 (&v)[N], int key, bool page_
 __device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
 
 // Products of KT key tiles: the running maximum m of every row, to which its sums l (this lane's part) and o are brought if it rises.
+// Then c is the factor that takes the products to scores less the maximum, fused.  A maximum is a product rounded after the factor, and the fused
+// s c - m leaves what that rounding took: nothing to speak of near 0, but from 2^31 on more than the exponents there are, so that a row's own
+// largest key would get 0 or infinity.  So once a maximum is beyond kFar (far: a bit for each lane), the products are rounded as it was and c is 1.
 template <int KT, int NT, int DT>
-__device__ __forceinline__ void raise_maximum(const f32x4 (&s)[KT][NT], float c, float (&m)[NT], float (&l)[NT], f32x4 (&o)[DT][NT])
+__device__ __forceinline__ void raise_maximum(f32x4 (&s)[KT][NT], float scale, float &c, unsigned long long &far, float (&m)[NT], float (&l)[NT], f32x4 (&o)[DT][NT])
 {
     float top[NT];
     bool rise = false;
@@ -535,10 +539,10 @@ __device__ __forceinline__ void raise_maximum(const f32x4 (&s)[KT][NT], float c,
         top[n] = max3(top[n], s[0][n][2], s[0][n][3]);
 #pragma unroll
         for (int b = 1; b < KT; ++b) top[n] = max3(max3(top[n], s[b][n][0], s[b][n][1]), s[b][n][2], s[b][n][3]);
-        top[n] *= c;
+        top[n] *= scale;
         rise |= top[n] > m[n] + kRise;
     }
-    if (__any(rise)) {
+    if (__ballot(rise) | far) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const float next = fmaxf(m[n], max_over_groups(top[n])), f = exp2_fast(m[n] - next);
@@ -546,6 +550,14 @@ __device__ __forceinline__ void raise_maximum(const f32x4 (&s)[KT][NT], float c,
             l[n] *= f;
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d][n] *= f;
+            far |= __ballot(fabsf(next) > kFar && next != kNothing);
+        }
+        if (far) {
+            c = 1.f;
+#pragma unroll
+            for (int b = 0; b < KT; ++b)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) s[b][n] *= scale;
         }
     }
 }
@@ -649,6 +661,8 @@ template <int D, bool FP8, int NT, int RG> __device__ __forceinline__ void few_r
         q.load(a, t, p.head, WROWS * rg, lane);
         f32x4 o[D / 16][NT];
         float m[NT], l[NT];
+        float c = q.c;
+        unsigned long long far = 0;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             m[n] = kNothing;
@@ -714,9 +728,9 @@ template <int D, bool FP8, int NT, int RG> __device__ __forceinline__ void few_r
                         }
                     if (again) load_k(at, h);
                     if (partly) mask<8, NT>(s, key + 8 * h, page_ok, q.k_min, q.k_max);
-                    raise_maximum(s, q.c, m, l, o);
+                    raise_maximum(s, q.c, c, far, m, l, o);
                     u32x4 pr[NT];
-                    probabilities(s, q.c, m, l, pr);
+                    probabilities(s, c, m, l, pr);
 #pragma unroll
                     for (int d = 0; d < D / 16; ++d) {
                         const u32x4 x = FP8 ? widen_half(v[d], h) : v[d];
@@ -814,6 +828,8 @@ template <int D, bool FP8> __device__ __forceinline__ void many_rows(const dx_at
         const tile_rows mine = see(a, job.of, idle ? t.first : t.first + WROWS * wave, WROWS);
         f32x4 o[D / 16][NT];
         float m[NT], l[NT];
+        float c = q.c;
+        unsigned long long far = 0;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             m[n] = kNothing;
@@ -919,7 +935,7 @@ template <int D, bool FP8> __device__ __forceinline__ void many_rows(const dx_at
 #pragma unroll
                 for (int u = 0; u < NU; ++u) mask<X, NT>(s + u * KT, (stage * NU + u) * UNIT + X * grp, page_ok[u], q.k_min, q.k_max);
             }
-            raise_maximum(s, q.c, m, l, o);
+            raise_maximum(s, q.c, c, far, m, l, o);
             // the sums in two halves: the second half's probabilities between the first one's products
             constexpr int PV = D / 16, PAIRS = 4 * NT;
             u32x4 v[2 * PV], pr[2][NT];
@@ -931,8 +947,8 @@ template <int D, bool FP8> __device__ __forceinline__ void many_rows(const dx_at
             auto pair = [&](int h, int j) {
                 if (j < PAIRS) {
                     const int n = j / 4, b = 2 * h + j / 2 % 2, i = 2 * (j % 2);
-                    e[j % 2][0] = exp2_fast(__builtin_fmaf(s[b][n][i], q.c, -m[n]));
-                    e[j % 2][1] = exp2_fast(__builtin_fmaf(s[b][n][i + 1], q.c, -m[n]));
+                    e[j % 2][0] = exp2_fast(__builtin_fmaf(s[b][n][i], c, -m[n]));
+                    e[j % 2][1] = exp2_fast(__builtin_fmaf(s[b][n][i + 1], c, -m[n]));
                 }
                 if (j > 0) {
                     const int x = j - 1, n = x / 4;

@@ -248,3 +248,49 @@ def test_attention_window_of_any_size(B, ctx, window):  # noqa: F811
             assert torch.isinf(got[1][:5]).all() and torch.isfinite(got[1][5:]).all()
 
 
+def far_scores(B, fmt, D, new, top, alike):  # noqa: F811
+    """Scores that are exact in fp32 and of the size of `top` (all alike, or key 0 alone far above the others), and the bounds for them:
+    nothing but probabilities of equal keys or of one key enters, whatever the scores' size."""
+    P = 16
+    c = Case(B, 4, 1, D, P, fmt, [new + 2], [new], seed=D + new)
+    half = 2.0 ** (math.frexp(abs(top))[1] // 2)
+    if fmt == "fp8":
+        c.ks.fill_(half)
+        code, k = 0x3F, 1.875 * half                             # (1.875 in e4m3)
+        low = 0x37 if top > 0 else 0x47                          # half of it, double
+        raw = c.ck
+    else:
+        code, k = 255 / 128 * half, 255 / 128 * half
+        low = code / 2 if top > 0 else code * 2
+        raw = c.ck.view(torch.bfloat16)
+    real = raw != 127 if fmt == "fp8" else ~torch.isnan(raw)
+    raw[real] = code if alike else low
+    c.k = torch.full_like(c.k, k if alike else k / 2 if top > 0 else k * 2)
+    page = int(c.table[0, 0])
+    raw[page, :, :, 0], c.k[page * P] = code, k                  # key 0
+    c.q[:] = 2.0 ** math.frexp(abs(top) / half)[1] / D * math.copysign(1, top) / 4
+    c.scale = 1.0
+    ref = R.attention(c.q.double(), c.k, c.v, c.table, c.q_offsets, c.lens, c.P, c.n_pages, c.scale, 0)
+    b_out, b_lse = R.attention_bounds(*ref[:3], torch.zeros_like(ref[3]), ref[4], D)
+    return c, ref, b_out, b_lse
+
+
+def check_far_scores(ctx, c, ref, b_out, b_lse):  # noqa: F811
+    out, lse = c.run(ctx)
+    assert torch.isfinite(lse).all() and torch.isfinite(out).all()
+    over = ((out.double() - ref[0]).abs() / b_out).max().item(), ((lse.double() - ref[1]).abs() / b_lse).max().item()
+    assert max(over) <= 1, over
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_attention_scores_far_from_zero(B, ctx, fmt, D, new):  # noqa: F811
+    """Beyond 2^31 half a unit in the last place of a score is more than the exponents there are."""
+    for top in (2.0 ** 20, 2.0 ** 30, 2.0 ** 35, 2.0 ** 60, 2.0 ** 120):
+        for sign in (1, -1):
+            for alike in (True, False):
+                print("far", fmt, D, new, top * sign, alike, flush=True)
+                check_far_scores(ctx, *far_scores(B, fmt, D, new, top * sign, alike))
+
+
