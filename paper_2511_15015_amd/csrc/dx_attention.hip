@@ -26,7 +26,7 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 #define DX_GLOBAL __attribute__((address_space(1)))
 
-constexpr float kNothing = -1.7e38f; // maximum of a row that has seen no key yet
+constexpr float kNothing = -3.402823466e38f; // maximum of a row that has seen no key yet: the lowest number
 constexpr float kRise = 8.f;
 constexpr float kFar = 16777216.f; // 2^24 (raise_maximum)
 constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;

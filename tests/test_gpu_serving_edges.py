@@ -294,3 +294,12 @@ def test_attention_scores_far_from_zero(B, ctx, fmt, D, new):  # noqa: F811
                 check_far_scores(ctx, *far_scores(B, fmt, D, new, top * sign, alike))
 
 
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_attention_scores_near_the_lowest_number(B, ctx, D, new):  # noqa: F811
+    """Every score is -1.98 * 2^126, -2.4e38 in base 2: a number still."""
+    case = far_scores(B, "bf16", D, new, -1.99 * 2.0 ** 127, True)
+    assert -2.0 ** 127 < case[1][1].min() <= case[1][1].max() < -1.9 * 2.0 ** 126
+    check_far_scores(ctx, *case)
+
+
