@@ -86,7 +86,7 @@ __device__ f32x4 mfma(const u32x4 &a, const u32x4 &b, const f32x4 &c)
 // stretch from the lengths (the host does not know them), and of a tile that it has a part of the line of, the same part of the units.
 // A tile that lies in one stretch is written out by its block.  The others are joined: a stretch has at most two
 // unfinished tiles, one that it found begun (slot 2 * block) and one that it leaves (slot 2 * block + 1); for each there is an entry
-// in a.joint, at 2 * blockIdx and behind it.  Joining costs as much as some units, so a cut that close to either end of a tile is moved there.
+// in what the block leaves to k_join (a.left).  Joining costs as much as some units, so a cut that close to either end of a tile is moved there.
 constexpr int kFine = 16;
 // In units (k_keys: 32 or 64 keys) and stages (k_rows: 64): what a tile costs beside its units, the shortest stretch, and how far cuts
 // are moved.  Measured, us a pass, 2000 new tokens (32 heads on 4 of 128 channels: tiles of 1 to 32 stages): tiles at their units alone 108, with
@@ -414,7 +414,7 @@ template <class K> __device__ bool next_task(const dx_attn_args &a, const batch 
     if (first < last) {
         k.slot = 2L * (p.base + p.block) + (p.block > first ? 0 : 1);
         if (threadIdx.x == 0)
-            a.joint[2 * blockIdx.x + (p.block > first ? 0 : 1)] =
+            a.left[blockIdx.x].joint[p.block > first ? 0 : 1] =
                 dx_attn_joint{p.base + first, last - first + 1, k.t.token, k.t.first, k.t.rows, p.head, !K::FEW, p.block - first};
     }
     return true;
@@ -627,6 +627,176 @@ template <int D, bool FP8> struct pages {
     template <bool ONCE = false> __device__ static u32x4 value_piece(const DX_GLOBAL char *at, int d) { return read<ONCE>(at + 256 * d); }
 };
 
+// ---- values that are no numbers --------------------------------------------------------
+// The rows of a tile do not all see the same keys, and 0 times a value that is no number is NaN: what a later token brought (or one that has left a row's
+// window) reaches rows of its tile that do not see it.  The loops over the keys do not look for that.  A result that is NaN is looked into once it has been
+// stored, and computed again from the keys that its row sees, alone, where a hidden value can have been the cause: among the keys that some rows
+// see and others do not, and none that the row does see is NaN anyway.  k_join does that, for tiles that a block stored whole, too (dx_attn_odd): as a part of
+// few_rows and many_rows it takes registers from their loops (a chunk of 512 tokens beside 32 decoding 79 us a pass, 84 with; drafts in e4m3 60 and 63).
+// It need not be fast: 4096 tokens after 4001, one of them NaN, 102 ms, all of them 13 ms (whoever sees one is NaN rightly).
+__device__ float bf16_at(uint32_t two, int i) { return __uint_as_float(i ? two & 0xFFFF0000u : two << 16); }
+// NaN if it has been, or an element of v is
+__device__ __forceinline__ float nan_of(float x, const f32x4 &v) { return max3(max3(x, v[0], v[1]), v[2], v[3]); }
+
+// Attention of one row, the same in all lanes, over keys lo .. hi - 1: channel 64 i + lane in o[i].  c: scores in base 2 per product.  A lane to a key for the
+// scores, to a channel for the sums.
+template <int D, bool FP8>
+__device__ void one_row(const pages<D, FP8> &kv, const dx_bf16 *q, float c, float v_scale, int lo, int hi, float (&o)[D / 64])
+{
+    constexpr int X = FP8 ? 16 : 8;
+    const int lane = threadIdx.x & 63, in_page = (1 << kv.shift) - 1;
+    float m = kNothing, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) o[i] = 0.f;
+    for (int base = lo & ~63; base < hi; base += 64) {
+        const int key = base + lane, page = key < hi ? kv.table[key >> kv.shift] : -1;
+        const bool ok = key >= lo && kv.real(page);
+        float s = 0.f;
+        if (ok) {
+            const DX_GLOBAL char *at = kv.k + page * kv.page_bytes + (key & in_page) * 16;
+#pragma unroll 1
+            for (int x = 0; x < D / X; ++x) {
+                const u32x4 k = *reinterpret_cast<const DX_GLOBAL u32x4 *>(at + ((long)x << kv.shift) * 16);
+#pragma unroll
+                for (int h = 0; h < X / 8; ++h) {
+                    const u32x4 wide = FP8 ? widen_half(k, h) : k, by = reinterpret_cast<const u32x4 *>(q)[x * (X / 8) + h];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s = __builtin_fmaf(bf16_at(wide[e / 2], e % 2), bf16_at(by[e / 2], e % 2), s);
+                }
+            }
+        }
+        s = ok ? s * c : -INFINITY;
+        float top = s;
+        for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+        const float next = fmaxf(m, top), f = exp2_fast(m - next), p = exp2_fast(s - next);
+        float sum = p;
+        for (int x = 32; x; x >>= 1) sum += __shfl_xor(sum, x);
+        m = next;
+        l = l * f + sum;
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) o[i] *= f;
+        const unsigned long long seen = __ballot(ok);
+#pragma unroll 1
+        for (int g = 0; g < 64; g += X) {
+            const uint32_t see = (uint32_t)(seen >> g) & ((1u << X) - 1);
+            if (!see) continue;
+            const DX_GLOBAL char *at = kv.v + __builtin_amdgcn_readlane(page, g) * kv.page_bytes + ((long)(((base + g) & in_page) / X) * D + lane) * 16;
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) {
+                const u32x4 v = *reinterpret_cast<const DX_GLOBAL u32x4 *>(at + 1024 * i);
+#pragma unroll
+                for (int h = 0; h < X / 8; ++h) {
+                    const u32x4 wide = FP8 ? widen_half(v, h) : v;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float by = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(p), g + 8 * h + e));
+                        if (see >> (8 * h + e) & 1) o[i] = __builtin_fmaf(by, bf16_at(wide[e / 2], e % 2), o[i]);
+                    }
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) o[i] *= inverse(l, v_scale);
+}
+
+// The stored results of row `row` of a tile at 4 channels from d on.  All lanes of a wavefront call it, live: with a row.
+template <int D, bool FP8>
+__device__ void look_into(const dx_attn_args &a, const tile_rows &t, int b, int head, int row, int d, bool live)
+{
+    constexpr int X = FP8 ? 16 : 8, SIZE = 16 / X;
+    const pages<D, FP8> kv(a, b, head, t.hi);
+    // the keys of row r: from first_key on, up to in front of end_key
+    auto first_key = [&](int r) { return a.window ? window_from(a, t.pos + by_group(a, t.first + r)) : 0; };
+    auto end_key = [&](int r) { return min(t.pos + by_group(a, t.first + r) + 1, t.hi); };
+    dx_bf16 *const out = row_at(a, t.token, head, t.first + row).out;
+    uint32_t nan = 0, redo = 0; // a bit for each channel
+    if (live) {
+        const u32x2 is = *reinterpret_cast<const u32x2 *>(out + d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) nan |= (uint32_t)((is[e / 2] >> 16 * (e % 2) & 0x7FFF) > 0x7F80) << e;
+    }
+    if (nan) {
+        const int lo = first_key(row), hi = end_key(row);
+#pragma unroll 1
+        for (int key = t.lo; key < t.hi; ++key) {
+            if (key >= t.all_lo && key < t.all_hi) { // every row sees it
+                key = t.all_hi - 1;
+                continue;
+            }
+            const int page = kv.table[key >> kv.shift], off = key & ((1 << kv.shift) - 1);
+            if (!kv.real(page)) continue;
+            const DX_GLOBAL char *at = kv.v + page * kv.page_bytes + ((long)(off / X) * D + d) * 16 + off % X * SIZE;
+#pragma unroll 1
+            for (int e = 0; e < 4; ++e) {
+                const int x = FP8 ? (at[16 * e] & 0x7F) : (*reinterpret_cast<const DX_GLOBAL dx_bf16 *>(at + 16 * e) & 0x7FFF);
+                if (key < lo || key >= hi) redo |= (uint32_t)(x >= (FP8 ? 0x7F : 0x7F80)) << e;
+                else if (x > (FP8 ? 0x7E : 0x7F80)) nan &= ~(1u << e);
+            }
+        }
+        redo &= nan;
+    }
+    for (unsigned long long m; (m = __ballot(redo != 0));) {
+        const int r = __builtin_amdgcn_readlane(row, __ffsll(m) - 1), i = by_group(a, t.first + r);
+        const dx_bf16 *q = a.q + (long)(t.token + i) * a.q_stride + (long)(head * a.group + t.first + r - i * a.group) * D;
+        float o[D / 64];
+        one_row<D, FP8>(kv, q, a.scale * kLog2e * (FP8 ? a.cache.k_scale[head] : 1.f), FP8 ? a.cache.v_scale[head] : 1.f, first_key(r), end_key(r), o);
+        const bool mine = row == r;
+#pragma unroll 1
+        for (int x = 0; x < 4; ++x) {
+            const int channel = d + x;
+            float value = 0.f;
+#pragma unroll
+            for (int j = 0; j < D / 64; ++j) {
+                const float of = __shfl(o[j], channel & 63);
+                if (channel >> 6 == j) value = of;
+            }
+            if (mine && redo >> x & 1) out[channel] = (dx_bf16)pack_bf16(value, 0.f);
+        }
+        if (mine) redo = 0;
+    }
+}
+// (with one token, or with as many that see the same, there is nothing to look for)
+__device__ bool may_differ(const tile_rows &t) { return t.lo < t.all_lo || t.all_hi < t.hi; }
+// A wavefront has stored a result that is NaN, of the tile that p is at and has all of.
+template <class K> __device__ __forceinline__ void note_odd(const dx_attn_args &a, const stretch &p)
+{
+    if (threadIdx.x & 63) return;
+    dx_attn_odd &odd = a.left[blockIdx.x].odd[threadIdx.x >> 6];
+    const dx_attn_place at{p.head, p.b, p.tile};
+    if (!odd.rows) odd.first = at; // (cleared by this wavefront: take_place)
+    odd.last = at;
+    odd.paired = p.even < 0;
+    odd.rows = K::FEW ? -K::ROWS : K::ROWS;
+}
+// k_join: those tiles, from the first of them to the last on the line (all between are the block's own)
+template <int D> __device__ void look_into_odd(const dx_attn_args &a, const dx_attn_odd &odd)
+{
+    const int lane = threadIdx.x & 63, rows = abs(odd.rows);
+    for (dx_attn_place at = odd.first;;) {
+        const tokens of = batch::read(a, at.b);
+        const int all = of.n * a.group, tiles = of.n > 0 && (all <= a.few) == (odd.rows < 0) ? (all + rows - 1) / rows : 0;
+        if (at.tile < tiles) {
+            const tile_rows t = see(a, of, (odd.paired ? paired(at.tile, tiles, at.head) : at.tile) * rows, rows);
+#pragma unroll 1
+            for (int e = lane; may_differ(t) && e - lane < t.rows * (D / 4); e += 64) {
+                const bool live = e < t.rows * (D / 4);
+                const int row = min(e / (D / 4), t.rows - 1), d = e % (D / 4) * 4;
+                if (a.cache.fmt == DX_KV_E4M3) look_into<D, true>(a, t, at.b, at.head, row, d, live);
+                else look_into<D, false>(a, t, at.b, at.head, row, d, live);
+            }
+            if (at.head == odd.last.head && at.b == odd.last.b && at.tile == odd.last.tile) return;
+            ++at.tile;
+        } else { // the next request, of the next head
+            at.tile = 0;
+            if (++at.b == a.B) {
+                at.b = 0;
+                if (++at.head == a.cache.kv_heads) return;
+            }
+        }
+    }
+}
+
 // ---- few rows: the wavefronts of a block share the keys --------------------------------
 // Decoding and drafts: up to 16 NT RG rows for a request and kv head (more: several tiles).  Bound by reading the cache once: 64 requests of 500
 // to 8000 tokens, 4 heads of 128 channels, 550 MB, 92 us = 6.0 TB/s; one of 150 thousand, 2 of 256, 307 MB, 54 us = 5.7 TB/s; in e4m3 with 1 to 6
@@ -769,6 +939,7 @@ template <int D, bool FP8, int NT, int RG> __device__ __forceinline__ void few_r
             for (int d = 0; d < D / 16; ++d) *reinterpret_cast<f32x4 *>(&s_o[(wave * WROWS + 16 * n + col) * PITCH + 16 * d + 4 * grp]) = o[d][n] * f;
         }
         __syncthreads();
+        float nan = 0.f;
         for (int e = tid; e < t.rows * (D / 4); e += 256) {
             const int r = e / (D / 4), d = e % (D / 4) * 4, in = r % WROWS;
             f32x4 sum = {0.f, 0.f, 0.f, 0.f};
@@ -785,8 +956,10 @@ template <int D, bool FP8, int NT, int RG> __device__ __forceinline__ void few_r
                 const row_at to(a, t.token, p.head, t.first + r);
                 to.store(d, sum * inverse(all, v_scale));
                 if (d == 0) to.store_lse(top, all);
+                nan = nan_of(nan, sum);
             }
         }
+        if (__builtin_expect(__any(nan != nan), 0)) note_odd<K>(a, p);
         if (!advance<K>(a, n_of, p)) break;
         __syncthreads();
     }
@@ -978,6 +1151,7 @@ template <int D, bool FP8> __device__ __forceinline__ void many_rows(const dx_at
         }
         __builtin_amdgcn_s_setprio(0);
         const float v_scale = FP8 ? a.cache.v_scale[p.head] : 1.f;
+        float nan = 0.f;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             l[n] = sum_over_groups(l[n]);
@@ -991,10 +1165,14 @@ template <int D, bool FP8> __device__ __forceinline__ void many_rows(const dx_at
                 const row_at to(a, t.token, p.head, t.first + r);
                 const float f = inverse(l[n], v_scale);
 #pragma unroll
-                for (int d = 0; d < D / 16; ++d) to.store(16 * d + 4 * grp, o[d][n] * f);
+                for (int d = 0; d < D / 16; ++d) {
+                    to.store(16 * d + 4 * grp, o[d][n] * f);
+                    nan = nan_of(nan, o[d][n]);
+                }
                 if (grp == 0) to.store_lse(m[n], l[n]);
             }
         }
+        if (__builtin_expect(__any(nan != nan), 0)) note_odd<K>(a, p);
         if (!advance<K>(a, n_of, p)) break;
         __syncthreads();
     }
@@ -1004,13 +1182,15 @@ template <int D, bool FP8> __device__ __forceinline__ void many_rows(const dx_at
 // blocks of a launch to a compute unit, by their registers; what is left of a launch's tiles is joined by as many blocks
 template <int D, int NT> constexpr int kBlocks = D == 256 ? 1 : NT == 1 && D == 64 ? 4 : 2;
 
-// The block takes a place on a line (whose first block is place `base` of the launch): its own two entries of a.joint say nothing yet.
+// The block takes a place on a line (whose first block is place `base` of the launch): what it leaves says nothing yet.
 __device__ __forceinline__ void take_place(const dx_attn_args &a, stretch &p, int block, int blocks, int base)
 {
     p.block = block;
     p.blocks = blocks;
     p.base = base;
-    if (threadIdx.x < 2) a.joint[2 * blockIdx.x + threadIdx.x].n = 0; // (written later, if at all, by the same wavefront)
+    // (written later, if at all, by the same wavefront)
+    if (threadIdx.x < 2) a.left[blockIdx.x].joint[threadIdx.x].n = 0;
+    if (threadIdx.x % 64 == 0) a.left[blockIdx.x].odd[threadIdx.x / 64].rows = 0;
 }
 
 template <int D, bool FP8, int NT, int RG> __global__ __launch_bounds__(256, (kBlocks<D, NT>)) void k_keys(dx_attn_args a)
@@ -1087,7 +1267,9 @@ template <int D> __global__ __launch_bounds__(256) void k_join(dx_attn_args a)
     __shared__ __attribute__((aligned(16))) float s_sum[256][4];
     __shared__ float s_top[256], s_all[256];
     const int tid = threadIdx.x;
-    const dx_attn_joint joints[2] = {a.joint[2 * blockIdx.x], a.joint[2 * blockIdx.x + 1]};
+    const dx_attn_joint joints[2] = {a.left[blockIdx.x].joint[0], a.left[blockIdx.x].joint[1]};
+    const dx_attn_odd &odd = a.left[blockIdx.x].odd[uniform(tid >> 6)];
+    const int odd_rows = odd.rows;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
         const dx_attn_joint j = joints[e];
@@ -1097,6 +1279,7 @@ template <int D> __global__ __launch_bounds__(256) void k_join(dx_attn_args a)
         const int lg = items <= 1 ? 0 : items > 128 ? 8 : 32 - __clz(items - 1), wide = 1 << lg, sets = 256 >> lg; // wide: items at a time
         const int set = tid >> lg;
         const float v_scale = a.cache.fmt == DX_KV_E4M3 ? a.cache.v_scale[j.head] : 1.f;
+        float nan = 0.f;
         for (int base = 0; base < items; base += wide) {
             const int item = first + min(base + (tid & (wide - 1)), items - 1);
             const piece_of<D> piece(item, j.by_lanes);
@@ -1127,9 +1310,26 @@ template <int D> __global__ __launch_bounds__(256) void k_join(dx_attn_args a)
                 const row_at to(a, j.token, j.head, j.first + piece.row);
                 to.store(piece.d, sum * inverse(all, v_scale));
                 if (piece.d == 0) to.store_lse(top, all);
+                nan = nan_of(nan, sum);
             }
         }
+        if (__builtin_expect(__any(nan != nan), 0)) {
+            int b = 0; // whose tile it is
+            tokens of = batch::read(a, b);
+            while ((of.first != j.token || of.n * a.group < j.first + j.rows) && b + 1 < a.B) of = batch::read(a, ++b);
+            const tile_rows t = see(a, of, j.first, j.rows);
+            if (may_differ(t))
+#pragma unroll 1
+                for (int base = 0; base < items; base += wide) {
+                    const piece_of<D> piece(first + min(base + (tid & (wide - 1)), items - 1), j.by_lanes);
+                    const bool live = set == 0 && base + tid < items && piece.row < j.rows;
+                    const int row = min(piece.row, j.rows - 1);
+                    if (a.cache.fmt == DX_KV_E4M3) look_into<D, true>(a, t, b, j.head, row, piece.d, live);
+                    else look_into<D, false>(a, t, b, j.head, row, piece.d, live);
+                }
+        }
     }
+    if (__builtin_expect(odd_rows != 0, 0)) look_into_odd<D>(a, odd);
 }
 
 // Requests of up to so many rows (new tokens * group) for a kv head are few_rows', where the kinds of a call are not known beforehand.
@@ -1175,11 +1375,11 @@ size_t dxk_attention_scratch(int n_cu, char *base, dx_attn_args *a)
     };
     char *part = take(channels * DX_ATTN_ROWS * sizeof(float));
     char *ml = take(slots * DX_ATTN_ROWS * sizeof(float2));
-    char *joint = take(slots * sizeof(dx_attn_joint));
+    char *left = take(slots / 2 * sizeof(dx_attn_left));
     if (a) {
         a->part = reinterpret_cast<float *>(part);
         a->part_ml = reinterpret_cast<float2 *>(ml);
-        a->joint = reinterpret_cast<dx_attn_joint *>(joint);
+        a->left = reinterpret_cast<dx_attn_left *>(left);
         a->n_cu = n_cu;
     }
     return at;

@@ -253,9 +253,9 @@ struct dx_attn_args {
     float scale;
     // Tiles of rows whose keys several blocks share: two slots for every block of a launch of unfinished rows and their maxima and
     // sums, and an entry for each that says which belong together.
-    float *part;                 // [2 * blocks, DX_ATTN_ROWS, head_dim]
-    float2 *part_ml;             // [2 * blocks, DX_ATTN_ROWS]
-    struct dx_attn_joint *joint; // [2 * blocks], by block index
+    float *part;               // [2 * blocks, DX_ATTN_ROWS, head_dim]
+    float2 *part_ml;           // [2 * blocks, DX_ATTN_ROWS]
+    struct dx_attn_left *left; // [blocks], by block index
     int n_cu;
     int few; // requests of at most so many rows (new tokens * group) are taken by few_rows, the others by many_rows
     uint32_t group_mul;
@@ -265,6 +265,17 @@ constexpr int DX_ATTN_ROWS = 128; // most rows of a tile
 struct dx_attn_joint { // a tile that the blocks at places `block` .. `block + n - 1` share (n = 0: none): slots 2 block + 1, 2 (block + 1), 2 (block + 2) ..
     int block, n, token, first, rows, head; // first token of its request, first row in it, rows, kv head
     int by_lanes, me;                       // the rows are as the accumulators of many_rows hold them; which of the n this block is
+};
+struct dx_attn_place {
+    int head, b, tile; // on the line of a launch
+};
+struct dx_attn_odd { // tiles that a block has stored whole, with results that are NaN
+    dx_attn_place first, last;
+    int rows, paired; // rows of a tile (0: no such tile; negative: of few_rows); whether tiles are on the line in pairs
+};
+struct dx_attn_left { // what a block of few_rows or many_rows leaves to the block of its index of k_join
+    dx_attn_joint joint[2];
+    dx_attn_odd odd[4]; // of each wavefront
 };
 // bytes of scratch, and its parts in `a`
 size_t dxk_attention_scratch(int n_cu, char *base, dx_attn_args *a);

@@ -303,3 +303,52 @@ def test_attention_scores_near_the_lowest_number(B, ctx, D, new):  # noqa: F811
     check_far_scores(ctx, *case)
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+@pytest.mark.parametrize("heads,kv,D", [(8, 8, 64), (24, 8, 64), (32, 4, 128), (6, 1, 256)])
+def test_attention_values_that_are_no_numbers_reach_the_rows_that_see_them(B, ctx, fmt, heads, kv, D):  # noqa: F811
+    """NaN and infinities in values of the new tokens (and under a window of old ones): a row that does not see such a token is as
+    without it, one that does gets what the sum gives, in that channel and no other."""
+    P = 16
+    steps = [([150, 40], [3, 6], 0), ([333, 20], [61, 1], 0), ([300], [300], 0), ([700, 90], [130, 5], 100), ([500], [70], 33)]
+    steps += [([60, 33] * 40, [5, 1] * 40, 0), ([60, 33] * 35 + [400], [5, 2] * 35 + [400], 0)]      # more requests than a wavefront has lanes
+    if D == 128:
+        steps.append(([4070], [4070], 0))                        # several whole tiles to a block
+    for lens, new, window in steps:
+        c = Case(B, heads, kv, D, P, fmt, lens, new, seed=heads + lens[0])
+        rng = np.random.default_rng(lens[0])
+        odd = torch.zeros_like(c.v)                              # what is no number, by slot, head and channel
+        for b, n in enumerate(lens):
+            first = max(n - new[b] - (window or 1), 0)
+            for j in rng.choice(np.arange(first, n), min(7, n - first), replace=False):
+                slot, h, d = int(c.table[b, j // P]) * P + int(j) % P, int(rng.integers(kv)), int(rng.integers(D))
+                what, bits = [(math.inf, 0x7F80), (-math.inf, 0xFF80 - 65536), (math.nan, 0x7FC1)][int(rng.integers(3))]
+                if fmt == "fp8":
+                    what, bits = math.nan, int(rng.choice([127, 255]))
+                odd[slot, h, d] = what
+                c.cv[slot // P, h, slot % P // c.X, d, slot % c.X] = bits
+                c.v[slot, h, d] = 0
+        print("no numbers", fmt, heads, kv, D, lens, new, window, flush=True)
+        out, lse = c.run(ctx, window)
+        ref = R.attention(c.q.double(), c.k, c.v, c.table, c.q_offsets, c.lens, P, c.n_pages, c.scale, window)
+        b_out, b_lse = R.attention_bounds(*ref, D)
+        want = ref[0].clone()
+        for b, n in enumerate(lens):
+            j = np.arange(n)
+            slot = torch.from_numpy(c.table[b, j // P] * P + j % P).cuda()
+            pos = torch.arange(n - new[b], n, device="cuda")[:, None]
+            jt = torch.from_numpy(j).cuda()
+            see = ((jt <= pos) & ((jt > pos - window) if window else (jt >= 0))).double()
+            for h in range(heads):
+                x = odd[slot, h // (heads // kv)]
+                up, down = see @ (~(x < 0) & (x != 0)).double(), see @ (~(x > 0) & (x != 0)).double()      # (NaN: both)
+                rows = want[c.q_offsets[b]:c.q_offsets[b + 1], h]
+                rows[(up > 0) & (down == 0)] = math.inf
+                rows[(up == 0) & (down > 0)] = -math.inf
+                rows[(up > 0) & (down > 0)] = math.nan
+        fine = torch.isfinite(want)
+        assert not fine.all() and torch.isfinite(lse).all()
+        assert ((out.double() - want).abs() <= b_out)[fine].all(), ((out.double() - want).abs() / b_out)[fine].max()
+        assert torch.equal(torch.nan_to_num(out.double(), 7.0, 8.0, 9.0)[~fine], torch.nan_to_num(want, 7.0, 8.0, 9.0)[~fine])
+        assert ((lse.double() - ref[1]).abs() <= b_lse).all()
+
+
