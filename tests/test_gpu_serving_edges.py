@@ -352,3 +352,21 @@ def test_attention_values_that_are_no_numbers_reach_the_rows_that_see_them(B, ct
         assert ((lse.double() - ref[1]).abs() <= b_lse).all()
 
 
+# ---- a chunk beside more requests than a wavefront has lanes -----------------------------------------------------------
+@pytest.mark.parametrize("fmt", ["bf16", "fp8"])
+@pytest.mark.parametrize("heads,kv,D", [(8, 2, 64), (16, 4, 128), (6, 1, 256)])
+@pytest.mark.parametrize("n", [65, 257, 1000])
+def test_attention_chunks_beside_many_requests(B, ctx, fmt, heads, kv, D, n):  # noqa: F811
+    """Chunks of several tiles at the first, a middle and the last request, requests without tokens between."""
+    rng = np.random.default_rng(n + D)
+    for chunks, window in (({0: 301}, 0), ({n // 2: 133}, 50), ({n - 1: 402}, 0), ({0: 77, n // 2: 250, n - 1: 129}, 0)):
+        new = [chunks.get(b, int(rng.integers(0, 3))) for b in range(n)]
+        lens = [max(x, 1) + int(rng.integers(0, 60)) for x in new]
+        for b in rng.choice(n, n // 10, replace=False):
+            if b not in chunks:
+                new[b], lens[b] = 0, int(rng.integers(0, 2)) * 9
+        print("chunks", fmt, heads, kv, D, n, chunks, window, flush=True)
+        c = Case(B, heads, kv, D, 16, fmt, lens, new, seed=n)
+        c.check(c.run(ctx, window), window)
+
+
