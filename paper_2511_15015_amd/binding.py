@@ -180,7 +180,7 @@ _int32 = _float32 = _bfloat16 = None  # torch's dtypes, once load() has imported
 def _typed(t, dtype):
     if t is None:
         return None
-    assert t.dtype is dtype and t.is_contiguous(), f"a contiguous tensor of {dtype} is needed"
+    assert t.dtype is dtype and t.is_cuda and t.is_contiguous(), f"a contiguous tensor of {dtype} on the device is needed"
     return t.data_ptr()
 
 
@@ -194,7 +194,7 @@ def _f32(t):
 
 def _rows(t, T, heads, D):
     """Address of T rows of [heads, D] bf16, contiguous but for the stride from row to row, and that stride."""
-    assert t.shape == (T, heads, D) and t.dtype is _bfloat16
+    assert t.shape == (T, heads, D) and t.dtype is _bfloat16 and t.is_cuda, "bf16 rows of [heads, channels] on the device are needed"
     assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == D), "heads and channels must be contiguous"
     return t.data_ptr(), t.stride(0) if T > 1 else heads * D
 
@@ -218,7 +218,9 @@ def make_kv_cache(k, v, k_scale=None, v_scale=None) -> DxKvCache:
     D = chunks * X
     assert k.dtype is v.dtype and k.dtype in (torch.bfloat16, torch.float8_e4m3fn) and X * k.element_size() == 16
     assert v.shape == (n_pages, kv_heads, page_size // X, D, X) and k.is_contiguous() and v.is_contiguous()
+    assert k.is_cuda and v.is_cuda, "the cache must be on the device"
     fp8 = k.dtype is torch.float8_e4m3fn
+    assert not fp8 or (k_scale is not None and v_scale is not None), "an e4m3 cache needs scales"
     assert not fp8 or k_scale.numel() == v_scale.numel() == kv_heads
     return DxKvCache(k.data_ptr(), v.data_ptr(), _f32(k_scale) if fp8 else None, _f32(v_scale) if fp8 else None,
                      kv_heads, D, page_size, n_pages, DX_KV_E4M3 if fp8 else DX_KV_BF16, 0)
@@ -496,8 +498,8 @@ class Context:
         B, stride = table.shape
         assert D == cache.head_dim and lens.numel() == B and q_offsets.numel() == B + 1
         if lse is not None:
-            assert lse.shape == (T, heads) and lse.dtype is _float32 and lse.is_contiguous()
-            lse = lse.data_ptr()
+            assert lse.shape == (T, heads)
+            lse = _f32(lse)
         s = self.lib.dx_paged_attention(self.h, cache, *_rows(q, T, heads, D), heads, _i32(q_offsets), _i32(lens), _i32(table),
                                         stride, B, T, max_q, scale, window, *_rows(out, T, heads, D), lse)
         if s:
