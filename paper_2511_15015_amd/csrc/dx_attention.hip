@@ -310,6 +310,7 @@ struct stretch {
     int base;
     int head, b, tile; // a tile of it, and where that starts on the line
     long start;
+    long end; // this block has none of the tiles that start behind it
     request r;
     // the blocks that have a part of the tile
     __device__ int first_block() const { return (int)min((start + near + share - 1) / share - 1, (long)blocks - 1); }
@@ -326,6 +327,7 @@ template <class K> __device__ bool locate(const dx_attn_args &a, const batch &n,
     p.near = l.even ? 1 : K::NEAR * kFine;
     const long at = max(p.block * p.share - p.near, 0L);
     if (at >= line) return false;
+    p.end = min((p.block + 1) * p.share - p.near, line - 1); // (first_block)
     p.head = uniform((int)(at / l.total));
     long in = at - p.head * l.total; // of the head's requests, then of one, then of a tile
     if (n.in_lanes) {
@@ -364,20 +366,32 @@ template <class K> __device__ bool locate(const dx_attn_args &a, const batch &n,
     return true;
 }
 
-// the tile behind; false: there is none
+// the tile behind; false: there is none, or it is another block's
 template <class K> __device__ bool advance(const dx_attn_args &a, const batch &n, stretch &p)
 {
     p.start += p.r.length(p.tile);
+    if (p.start > p.end) return false;
     if (++p.tile < p.r.tiles) return true;
     p.tile = 0;
-    do {
-        if (++p.b == a.B) {
-            p.b = 0;
+    // The next request that has some, 64 looked at at once.  Looked at one after another, us a pass, and so: 3 live requests of 1024 254 and 21 (of 3:
+    // 11), a chunk of 512 tokens beside 999 decoding 387 and 168.  (They are not all without tiles: then there is no line.)
+    const int lane = threadIdx.x & 63;
+    for (int from = p.b + 1;;) {
+        const int at = n.in_lanes ? lane : from + lane;
+        const tokens of = n.in_lanes ? n.mine : at < a.B ? batch::read(a, at) : tokens{0, 0, 0};
+        const unsigned long long some = __ballot(at >= from && of.n > 0 && (of.n * a.group <= a.few) == K::FEW);
+        if (some) {
+            const int in = __ffsll(some) - 1;
+            p.b = n.in_lanes ? in : from + in;
+            p.r = make_request<K>(a, tokens{__builtin_amdgcn_readlane(of.first, in), __builtin_amdgcn_readlane(of.n, in), __builtin_amdgcn_readlane(of.len, in)}, p.even);
+            return true;
+        }
+        from += 64;
+        if (n.in_lanes || from >= a.B) {
+            from = 0;
             if (++p.head == a.cache.kv_heads) return false;
         }
-        p.r = make_request<K>(a, n.get(a, p.b), p.even);
-    } while (p.r.tiles == 0); // (the requests are not all without tiles: then there is no line)
-    return true;
+    }
 }
 
 // What a block does next: a tile, some units of it, and where its rows go.

@@ -370,3 +370,32 @@ def test_attention_chunks_beside_many_requests(B, ctx, fmt, heads, kv, D, n):  #
         c.check(c.run(ctx, window), window)
 
 
+@pytest.mark.parametrize("live", ["first", "last", "spread"])
+def test_attention_places_without_a_request_cost_next_to_nothing(B, ctx, live):  # noqa: F811
+    """4 live requests in 1024 places against the same 4 alone, which is bound by latency: no block may walk over the others.  (Four
+    times as long is allowed; a walk takes twenty times as long.)"""
+    n = 1024
+    at = {"first": [0, 1, 2, 3], "last": [n - 4, n - 3, n - 2, n - 1], "spread": [5, 300, 301, 900]}[live]
+    times = []
+    for places in (4, n):
+        where = range(4) if places == 4 else at
+        lens, new = [0] * places, [0] * places
+        for b in where:
+            lens[b], new[b] = 400, 1
+        c = Case(B, 32, 4, 128, 16, "bf16", lens, new, seed=1)
+        c.check(c.run(ctx))
+        args = c.cache, c.q, dev(c.q_offsets), dev(c.lens), dev(c.table), 1, c.scale, 0, torch.empty_like(c.q)
+        took = []
+        for _ in range(7):
+            start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            start.record()
+            for _ in range(20):
+                ctx.dx_paged_attention(*args)
+            end.record()
+            torch.cuda.synchronize()
+            took.append(start.elapsed_time(end) / 20)
+        times.append(sorted(took)[3])
+    print("places", live, times, flush=True)
+    assert times[1] <= 4 * times[0], times
+
+
