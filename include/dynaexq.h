@@ -446,9 +446,11 @@ typedef struct {
 /* One-time scratch of the calls below for up to max_requests requests in a step (at
  * most 4096) and heads of up to max_head_dim channels: the unfinished sums of keys
  * that several blocks share, and of the chunks of a row of dx_draft_verify.  Before it
- * those calls return DX_ERR_INVALID, a second one returns DX_ERR_BUSY.  Synchronises
- * the compute stream.  The calls run on that stream and share the scratch, so those on
- * one context must not overlap. */
+ * those calls return DX_ERR_INVALID (but dx_kv_write, which needs none), a second one
+ * returns DX_ERR_BUSY.  max_head_dim bounds what dx_paged_attention takes; the scratch
+ * is as large for each (the more channels, the fewer blocks).  Synchronises the compute
+ * stream.  The calls run on that stream and share the scratch, so those on one context
+ * must not overlap. */
 dx_status dx_serve_reserve(dx_ctx *ctx, int max_requests, int max_head_dim);
 
 /* Pages and slots of a step.  All arrays dev int32.
@@ -502,13 +504,15 @@ dx_status dx_kv_write(dx_ctx *ctx, const dx_kv_cache *cache, const void *k_bf16,
  *   s_j = scale * (q . k_j),  p = softmax(s),  out = sum_j p_j v_j,  lse = ln sum_j exp(s_j)
  * Query head h reads kv head h / (q_heads / kv_heads).  A row that sees no key (lens[b] < n), gets out = 0 and
  * lse = -inf.  Keys past lens[b] and keys of a page that is none (outside 0 .. n_pages-1) are not seen,
- * whatever the memory holds.
+ * whatever the memory holds, and a NaN or infinity reaches the rows that see its key, no others.  Rows of q past
+ * q_offsets[B] are padding: their out and lse stay as they are.
  *   q, out dev bf16: row of token t at q + t * q_stride (elements), [q_heads, head_dim]; lse dev fp32
  *   [T, q_heads] or NULL; q_offsets [B+1], lens [B], table [B, table_stride] dev int32, as dx_pages_plan
  *   writes them.  max_q: the most new tokens of a request, a hint for the choice of kernels (more are
  *   computed all the same, slower).
- * bf16 products, sums and softmax in fp32; probabilities are rounded to bf16 for their product with the values
- * (relative error up to 2^-8 each).  A repeated call gives the same bits.  Starts at multiples of 16 bytes (lse: 4),
+ * bf16 products, sums and softmax in fp32 (scores beyond 2^127 are infinite); probabilities are rounded to bf16 for their
+ * product with the values (relative error up to 2^-8 each).  A repeated call gives the same bits.  out and lse overlap none of the
+ * inputs.  Starts at multiples of 16 bytes (lse: 4),
  * strides of multiples of 8.  kv_heads <= 1024 divides q_heads <= 1024; table_stride * page_size and T * q_heads at most
  * 2^30; head_dim up to that of dx_serve_reserve; B and T as in dx_pages_plan; scale finite. */
 dx_status dx_paged_attention(dx_ctx *ctx, const dx_kv_cache *cache, const void *q_bf16, int64_t q_stride,

@@ -89,7 +89,7 @@ __device__ f32x4 mfma(const u32x4 &a, const u32x4 &b, const f32x4 &c)
 // in what the block leaves to k_join (a.left).  Joining costs as much as some units, so a cut that close to either end of a tile is moved there.
 constexpr int kFine = 16;
 // In units (k_keys: 32 or 64 keys) and stages (k_rows: 64): what a tile costs beside its units, the shortest stretch, and how far cuts
-// are moved.  Measured, us a pass, 2000 new tokens (32 heads on 4 of 128 channels: tiles of 1 to 32 stages): tiles at their units alone 108, with
+// are moved.  Measured as each was set, in bf16 (the same numbers for e4m3 and other heads), us a pass, 2000 new tokens (32 heads on 4 of 128 channels: tiles of 1 to 32 stages): tiles at their units alone 108, with
 // 2, 3, 4 stages more 77, 75, 74; cuts moved over 4, 8, 12 stages without that 108, 95, 85, but 512 tokens after 8000 105, 110, 119.
 // Stretches of at least 6 and 4 stages: 300 new tokens 25.9 and 21.7, 100 after 1500 30.3 and 29.6, 9 requests with prompts of 9 to 300 27.8 and 26.8.
 constexpr int kKeysOver = 6, kKeysMin = 8, kKeysNear = 4, kRowsOver = 4, kRowsMin = 4, kRowsNear = 3;
@@ -235,7 +235,7 @@ template <class K> __device__ int even_units(const dx_attn_args &a, const batch 
 // Tiles of a single request are not cut where so many whole ones to a block, the longest and the shortest in pairs, take no more than K::WHOLE units
 // above an equal share of all: a cut is two parts of 128 rows written and read again.  The pairs are as long as each other, and stay
 // together from head to head if every other head's order is turned round.  Returns minus that number, or 0.  Measured, us a pass, cut and whole,
-// 32 heads on 4 of 128 channels: 512 new tokens 31.9 and 26.8, 4001 162 and 140, 4096 after 4001 404 and 379, 8192 547 and 519; where
+// 32 heads on 4 of 128 channels, a call of one request (of eight places, seven of them idle, 4096 after 4001 418): 512 new tokens 31.9 and 26.8, 4001 162 and 140, 4096 after 4001 404 and 379, 8192 547 and 519; where
 // they are cut anyway the look costs 0.4.  At WHOLE = 16 also 1024 tokens 37.8 and 41.2.
 template <class K> __device__ int whole_tiles(const dx_attn_args &a, const request &r, int blocks)
 {
@@ -247,7 +247,8 @@ template <class K> __device__ int whole_tiles(const dx_attn_args &a, const reque
 // even (make_request) for a single request, of which r is the line: as many parts of a tile as the blocks allow, unless that leaves them longer than an
 // equal share, what a tile costs beside its units included, by more than K::MORE.  (All lanes get here; lane 0 has the request.)  Measured, us a
 // pass, without and with: 100 tokens after 3000, 32 heads on 4 of 128 channels, 31 and 26.4, 201 after 16000 86 and 78, 512 after 8000 90 and 82,
-// 501 after 200, 256 channels, 47 and 32 (before the join went by XCD); at MORE = 3 301 after 9000 68 and 66; where it is not taken it costs 0.3.
+// 501 after 200, 256 channels, 47 and 32; at MORE = 3 301 after 9000 68 and 66; where it is not taken it costs 0.3 (measured while the join still went
+// by the place on the line: 501 tokens now 28.6).
 template <class K> __device__ int even_tiles(const dx_attn_args &a, const batch &n, const request &r, int blocks)
 {
     const int units = make_request<K>(a, n.mine, 1).first / kFine; // of the longest tile
@@ -318,7 +319,7 @@ struct stretch {
 };
 
 // Puts p at the first tile of its block, or at one in front of it: stretches of at least MIN units, cuts moved over up to NEAR.  All threads of
-// the block call it; s_found: 6 words of LDS.  False: there is none.
+// the block call it; s_found: 3 words of LDS.  False: there is none.
 template <class K> __device__ bool locate(const dx_attn_args &a, const batch &n, const line_part &l, stretch &p, int *s_found)
 {
     const long line = l.total * a.cache.kv_heads;
@@ -575,7 +576,9 @@ __device__ __forceinline__ void raise_maximum(f32x4 (&s)[KT][NT], float scale, f
         }
     }
 }
-// Products of two key tiles to probabilities, an operand of the product with the values; adds them to l.
+// Products of two key tiles to probabilities, an operand of the product with the values; adds them to l.  They are rounded to bf16, the type that the
+// values of a bf16 cache have in that product (2^-8 of a probability at most; the results are 0.0023 from 64 bits, 0.0017 with probabilities in
+// 32 bits); l takes them as they were.  Values in e4m3 would fit f16 probabilities, too, at the same number of instructions.
 template <int NT> __device__ __forceinline__ void probabilities(const f32x4 (*s)[NT], float c, const float (&m)[NT], float (&l)[NT], u32x4 (&pr)[NT])
 {
 #pragma unroll
@@ -813,8 +816,8 @@ template <int D> __device__ void look_into_odd(const dx_attn_args &a, const dx_a
 
 // ---- few rows: the wavefronts of a block share the keys --------------------------------
 // Decoding and drafts: up to 16 NT RG rows for a request and kv head (more: several tiles).  Bound by reading the cache once: 64 requests of 500
-// to 8000 tokens, 4 heads of 128 channels, 550 MB, 92 us = 6.0 TB/s; one of 150 thousand, 2 of 256, 307 MB, 54 us = 5.7 TB/s; in e4m3 with 1 to 6
-// new tokens also by the vector instructions (45 % of the time, the products 20 %): 33 requests, 227 MB, 49 us = 4.6 TB/s.
+// to 8000 tokens, 4 heads of 128 channels, 550 MB, 92 us = 6.0 TB/s; one of 150 thousand, 2 of 256, 307 MB, 53 us = 5.8 TB/s; in e4m3 with 1 to 6
+// new tokens also by the vector instructions (47 % of the time, the products 20 %): 33 requests, 227 MB, 51 us = 4.5 TB/s.
 // The four wavefronts are as many groups of 16 NT rows as the tile needs, 1 to RG, times takers of units in turn.  Keys and values of a wavefront's next
 // unit are loaded into the registers that the scores, and the sums, have just been taken from: two wavefronts to a SIMD
 // keep the memory busy in each other's computation.  At the end of a tile the takers join their sums through LDS.
@@ -984,7 +987,8 @@ template <int D, bool FP8, int NT, int RG> __device__ __forceinline__ void few_r
 // are (1 KB pieces, a lane's 16 bytes at 16 * lane: no bank conflicts), two stages in turn with one barrier each.  The next
 // stage is on its way meanwhile: bf16 straight to LDS, fp8 to registers, to be widened before it is stored.  Bound by the instructions of
 // the products (1024 cycles of a wavefront's stage) and of the softmax (1040), which two wavefronts to a SIMD run side by side only in part: 4096
-// tokens after 4001, 32 heads of 128 channels, 4.06e11 operations, 379 us = 1.07 PFLOP/s (a library's product of 8192^3 1.1 to 1.4).
+// tokens after 4001, 32 heads of 128 channels, 4.06e11 operations, 378 us = 1.07 PFLOP/s (a library's product of 8192^3 1.12 the same day, 1.37 on
+// another); 2000 tokens after 1000, 16 heads of 256 channels 134 us = 0.49, in e4m3 146 = 0.45, 32 of 128 in e4m3 104 = 0.63, 4000 after 1000, 16 of 64 90 = 0.55.
 template <int D, bool FP8> struct many {
     static constexpr int X = FP8 ? 16 : 8, UNIT = 4 * X, STAGE = 64, NU = STAGE / UNIT; // keys, units of a stage
     static constexpr int PIECES = NU * (D / 8), WIDE = FP8 ? 2 : 1;                     // 16-byte pieces of a stage, operands of a piece
@@ -1242,7 +1246,7 @@ template <int D, bool FP8> __global__ __launch_bounds__(256, (kBlocks<D, 2>)) vo
 
 // Both kinds in one launch (chunks of prompts beside decoding requests): the first blocks take the requests of few rows, which are
 // bound by memory, the others those of many, which are not, so that each has the half that the other leaves.  They are as many as
-// the lines are long, a stage of many rows taking as long as kStage units of few.  A chunk of 512 tokens beside 32 decoding requests of 1000
+// the lines are long, a stage of many rows taking as long as kStage units of few (set at 32 heads on 4 of 128 channels in bf16).  A chunk of 512 tokens beside 32 decoding requests of 1000
 // to 6000, 32 heads on 4 of 128 channels, 78 us; one of 385 beside 8, 64 channels, a window of 1024, 25, of which the launch, the search
 // for the block's place and the first loads are more than half.
 constexpr int kStage = 2;
@@ -1274,7 +1278,7 @@ template <int D, bool FP8> __global__ __launch_bounds__(256, (kBlocks<D, 2>)) vo
 // Tiles whose keys several blocks shared.  As many blocks as shared a tile join it, each a part of its rows' channels, four channels to
 // a thread; where that leaves threads over, several take turns on the parts.  A block joins what the block of its index left, because that had the
 // same XCD, and with it, in k_rows, the tile's other blocks: their sums are in its L2 (joined by the place on the line: 501 tokens
-// after 200, 256 channels, 33 us a pass, 28.6 so; a chunk of 385 beside 8 decoding 27.6, 25.1).  Latency: 2 to 4.6 us if there is nothing to join, 3 to 6 else (one request
+// after 200, 256 channels, 33 us a pass, 28.6 so; a chunk of 385 beside 8 decoding 27.6, 25.1).  Latency: 2 to 4.8 us if there is nothing to join, 4 to 6 else (one request
 // of 150 thousand tokens, all blocks' parts of 16 heads of 256 channels, 4.6).
 template <int D> __global__ __launch_bounds__(256) void k_join(dx_attn_args a)
 {

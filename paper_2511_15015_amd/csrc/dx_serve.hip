@@ -13,7 +13,7 @@ namespace {
 // One block: prefix sums over the requests of pages returned, pages taken and new tokens, in LDS.  Then a thread deals with a
 // request's pages and tokens if they are few (decoding), and lists it otherwise; the listed ones are dealt out to the wavefronts by
 // 512 items, eight loads of a lane on their way together.  Bound by the latency of its dependent rounds of loads and
-// barriers: 1001 requests, 15 thousand pages returned and 8000 new tokens 19 us a pass, 32 requests 8.  (A bisection of the prefix sums for
+// barriers: 1001 requests, 15 thousand pages returned and 8000 new tokens 20 us a pass, 32 requests 8.  (A bisection of the prefix sums for
 // every item 44 and 9, eight of them side by side 40 and 17: that is bound by LDS.)
 constexpr int kPlanThreads = 1024, kMost = 1 << 22; // most pages, and new tokens, of a request (sums of a wavefront's in 32 bits)
 
